@@ -26,6 +26,7 @@
 // slower everywhere (no partials to combine in LDS), and fewer or more waves than the device
 // holds at once 2-50% slower.
 #include "attn_decode.h"
+#include "decode_runs.h"
 
 namespace tide {
 namespace kern {
@@ -33,39 +34,6 @@ namespace kern {
 constexpr int kStreamBig = 8, kStreamSmall = 4;  // waves per workgroup (stream_waves)
 
 typedef const __attribute__((address_space(4))) StreamItem const_item;
-
-// Rows of one unit being merged by a wave: lanes L j .. L j + L - 1 hold head j0 + j (64 / L
-// heads a pass), each lane D / L consecutive head-dim entries.  With M the largest m seen, acc
-// = sum 2^(m_s - M) o_s, l and lx the same sums of the bf16-rounded and the exact weights.
-template <int D, int L>
-struct RowMerge {
-  static constexpr int kPer = D / L, kV = kPer / 4;
-  f32x4 acc[kV];
-  float mx, l, lx;
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int k = 0; k < kV; ++k) acc[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    mx = kNoMax;
-    l = lx = 0.0f;
-  }
-  // makes `m` part of the running maximum
-  __device__ __forceinline__ void raise(float m) {
-    const float mn = fmaxf(mx, m), w = fast_exp2(mx - mn);
-#pragma unroll
-    for (int k = 0; k < kV; ++k) acc[k] *= w;
-    l *= w;
-    lx *= w;
-    mx = mn;
-  }
-  // adds a part whose maximum is included in mx already
-  __device__ __forceinline__ void add(f32x4 ml, const f32x4 (&o)[kV]) {
-    const float w = fast_exp2(ml[0] - mx);
-    l += w * ml[1];
-    lx += w * ml[2];
-#pragma unroll
-    for (int k = 0; k < kV; ++k) acc[k] += w * o[k];
-  }
-};
 
 template <int D, bool kAppend, int kWaves>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -413,80 +381,10 @@ void decode_stream_kernel(StreamArgs a) {
   __syncthreads();
   if (a.reads.done && threadIdx.x == 0) plan_read(a.reads, blockIdx.x);
 
-  // Merges every part of a task in key order and writes this head's rows.
-  auto merge = [&](auto lanes_tag, const StreamUnit& u, int task) {
-    constexpr int L = decltype(lanes_tag)::value;
-    using RM = RowMerge<D, L>;
-    constexpr int kB = 16 / RM::kV;  // parts loaded together
-    const int sub = lane % L;
-    const int np = stream_parts(u, kWaves);
-    for (int j0 = 0; j0 < G; j0 += 64 / L) {
-      const int j = j0 + lane / L;
-      const bool ok = j < G;
-      RM rm;
-      rm.clear();
-      for (int e0 = 0; e0 < np; e0 += kB) {
-        f32x4 ml[kB], po[kB][RM::kV];
-#pragma unroll
-        for (int i = 0; i < kB; ++i) {
-          const int e = e0 + i;
-          const bool in = e < np;
-          const int64_t slot = slot0 + stream_slot(u, slots, task, in ? e : 0);
-          const auto rml = __builtin_amdgcn_make_buffer_rsrc(
-              a.part_ml + slot * G * 4, 0, in ? G * 16 : 0, 0x00020000);
-          const auto rpo = __builtin_amdgcn_make_buffer_rsrc(
-              a.part_o + slot * G * D, 0, in ? G * D * 4 : 0, 0x00020000);
-          ml[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rml, 16 * j, 0, kDeviceScope));
-#pragma unroll
-          for (int k = 0; k < RM::kV; ++k)
-            po[i][k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                     rpo, 4 * (j * D + RM::kPer * sub + 4 * k), 0, kDeviceScope));
-        }
-        float m = kNoMax;
-#pragma unroll
-        for (int i = 0; i < kB; ++i) {
-          if (e0 + i >= np) ml[i][0] = kNoMax;
-          m = fmaxf(m, ml[i][0]);
-        }
-        rm.raise(m);
-#pragma unroll
-        for (int i = 0; i < kB; ++i) rm.add(ml[i], po[i]);
-      }
-      if (ok) {
-        const float inv = 1.0f / rm.l;
-        const int64_t row = (int64_t)task * a.num_q_heads + head * G + j;
-        uint16_t* orow = a.out + row * D + RM::kPer * sub;
-#pragma unroll
-        for (int k = 0; k < RM::kV; ++k) {
-          const uint2 x = {pack_bf16x2(rm.acc[k][0] * inv, rm.acc[k][1] * inv),
-                           pack_bf16x2(rm.acc[k][2] * inv, rm.acc[k][3] * inv)};
-          *reinterpret_cast<uint2*>(orow + 4 * k) = x;
-        }
-        if (a.lse && sub == 0) a.lse[row] = (rm.mx + __log2f(rm.lx)) * kLn2;
-      }
-    }
-  };
-  // Flags the part in `slot` complete; a part that then finds all of the task's flags set merges.
-  // Each flag is written (device scope, acknowledged) after the part's own stores and before
-  // it looks, so the part whose flag lands last finds them all; should two find them, both
-  // write the same rows.  Unlike a counter, the flags need no zeros to start from.
-  auto arrive = [&](const StreamUnit& u, int task, int64_t slot) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (lane == 0)
-      __hip_atomic_store(a.flags + slot, a.call, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    const int np = stream_parts(u, kWaves);
-    for (int e = lane; e - lane < np; e += 64) {
-      const int64_t other = slot0 + stream_slot(u, slots, task, min(e, np - 1));
-      if (__any(__hip_atomic_load(a.flags + other, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.call))
-        return;
-    }
-    asm volatile("" ::: "memory");
-    if (G > 4) merge(std::integral_constant<int, 8>(), u, task);
-    else merge(std::integral_constant<int, 16>(), u, task);
-  };
-
-  if (has_flush) arrive(flush, flush_task, slot0 + slots.ended(run, flush_task));
+  auto row_of = [&](int task, int j) { return (int64_t)task * a.num_q_heads + head * G + j; };
+  const RunParts<D, kWaves, decltype(row_of)> parts = {a.part_o, a.part_ml, a.flags, a.call, a.out,
+                                                      a.lse,    slots,     slot0,   G,      row_of};
+  if (has_flush) parts.arrive(flush, flush_task, slot0 + slots.ended(run, flush_task));
   if (!has_final) return;
   auto left_open = [&](int x) { return __builtin_amdgcn_readfirstlane(open_task[x]); };
   if (wave > 0 && left_open(wave - 1) == cu.task) return;  // the first of these waves goes on
@@ -494,52 +392,8 @@ void decode_stream_kernel(StreamArgs a) {
   while (wave + len < kWaves && left_open(wave + len) == cu.task) ++len;
   const StreamUnit u = stream_unit(run, begin, cu.step - begin, cu.steps, a.steps);
   const bool whole = !u.ends_inside && u.n == len;  // the unit lies inside this workgroup
-  auto combine = [&](auto lanes_tag) {
-    constexpr int L = decltype(lanes_tag)::value;
-    using RM = RowMerge<D, L>;
-    const int sub = lane % L;
-    for (int j0 = 0; j0 < G; j0 += 64 / L) {
-      const int j = j0 + lane / L;
-      const int jr = j < G ? j : 0;
-      RM rm;
-      rm.clear();
-      for (int x = 0; x < len; ++x) {
-        const uint8_t* xo = k_lds0 + (wave + x) * 2 * KL::kPageBytes + 4 * D * jr;
-        const f32x4 ml = *reinterpret_cast<const f32x4*>(k_lds1 + (wave + x) * 2 * KL::kPageBytes + 16 * jr);
-        f32x4 po[RM::kV];
-#pragma unroll
-        for (int k = 0; k < RM::kV; ++k)
-          po[k] = *reinterpret_cast<const f32x4*>(xo + 16 * ((RM::kV * sub + k) ^ jr));
-        rm.raise(ml[0]);
-        rm.add(ml, po);
-      }
-      if (j >= G) continue;
-      if (whole) {
-        const float inv = 1.0f / rm.l;
-        const int64_t row = (int64_t)cu.task * a.num_q_heads + head * G + j;
-        uint16_t* orow = a.out + row * D + RM::kPer * sub;
-#pragma unroll
-        for (int k = 0; k < RM::kV; ++k) {
-          const uint2 x = {pack_bf16x2(rm.acc[k][0] * inv, rm.acc[k][1] * inv),
-                           pack_bf16x2(rm.acc[k][2] * inv, rm.acc[k][3] * inv)};
-          *reinterpret_cast<uint2*>(orow + 4 * k) = x;
-        }
-        if (a.lse && sub == 0) a.lse[row] = (rm.mx + __log2f(rm.lx)) * kLn2;
-      } else {
-        const int64_t slot = slot0 + slots.open(run, cu.task);
-        float* po = a.part_o + slot * G * D;
-#pragma unroll
-        for (int k = 0; k < RM::kV; ++k)
-          store_f32x4_device(po, G * D * 4, 4 * (j * D + RM::kPer * sub + 4 * k), rm.acc[k]);
-        if (sub == 0)
-          store_f32x4_device(a.part_ml + slot * G * 4, G * 16, 16 * j,
-                             f32x4{rm.mx, rm.l, rm.lx, 0.0f});
-      }
-    }
-  };
-  if (G > 4) combine(std::integral_constant<int, 8>());
-  else combine(std::integral_constant<int, 16>());
-  if (!whole) arrive(u, cu.task, slot0 + slots.open(run, cu.task));
+  parts.close(k_lds0 + wave * 2 * KL::kPageBytes, k_lds1 + wave * 2 * KL::kPageBytes, 2 * KL::kPageBytes,
+              2 * KL::kPageBytes, len, whole, u, run, cu.task);
 }
 
 template <int D, bool kAppend>
