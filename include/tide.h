@@ -112,7 +112,13 @@ enum {
   TIDE_OP_KV_APPEND = 1,
   TIDE_OP_EXTEND = 2,
   TIDE_OP_DECODE = 3,
-  TIDE_OP_FULL_PREFILL = 4
+  TIDE_OP_FULL_PREFILL = 4,
+  TIDE_OP_KV4_APPEND = 5,
+  TIDE_OP_KV4_UNPACK = 6,
+  TIDE_OP_KV4_DECODE = 7, /* tide_kv4_decode_attn, tide_kv4_decode_append_attn */
+  TIDE_OP_KV4_EXTEND = 8,
+  TIDE_OP_ATTN_MASS = 9, /* tide_attn_mass, tide_kv4_attn_mass */
+  TIDE_OP_KV_EVICT = 10  /* tide_kv_evict, tide_kv4_evict */
 };
 
 /* Attention shape shared by all calls. */
@@ -129,6 +135,10 @@ typedef struct tide_dims {
  *   op == TIDE_OP_KV_APPEND / TIDE_OP_EXTEND: lens_a = prefix_lens, lens_b = extend_lens
  *   op == TIDE_OP_DECODE:                     lens_a = kv_lens,     lens_b ignored
  *   op == TIDE_OP_FULL_PREFILL:               lens_a = seq_lens,    lens_b ignored
+ *   op == TIDE_OP_KV4_APPEND / TIDE_OP_KV4_UNPACK / TIDE_OP_KV4_EXTEND / TIDE_OP_ATTN_MASS:
+ *                                             lens_a = prefix_lens, lens_b = extend_lens
+ *   op == TIDE_OP_KV4_DECODE:                 lens_a = kv_lens,     lens_b ignored
+ *   op == TIDE_OP_KV_EVICT:                   lens_a = kv_lens,     lens_b = keep_lens
  * num_splits is used by TIDE_OP_DECODE only (0 = automatic; see tide_decode_attn).
  * The size depends only on the arguments, never on device state.
  */
@@ -307,6 +317,142 @@ TIDE_API int tide_full_prefill_attn(const void* q, const void* k_pool, const voi
                            int32_t num_tasks, const int32_t* seq_lens, const tide_dims* dims,
                            void* out, float* lse, void* workspace, size_t workspace_bytes,
                            void* stream);
+
+/* ---- the 4-bit cache ----------------------------------------------------------------------
+ *
+ * A pool that holds K and V in 4 bits keeps 3.8 times the tokens of a bf16 pool in the same
+ * memory, so more paused tasks stay resident (Section 4.2) and decode reads that much less.
+ * Format.  The d values of a token's K (or V) row of one KV head form blocks of 32.  A block holds
+ * a scale 2^s and 32 codes in e2m1 (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives; code = sign
+ * bit, 2 exponent bits, 1 mantissa bit).  s is the least integer in [-120, 125] with
+ * max|x| <= 7 * 2^s (125 if there is none); codes are x / 2^s to nearest, ties to the even
+ * code, at most 6 in magnitude.  Every code times its scale is exact in bf16.  A block with a NaN
+ * or an infinity reads back as NaN in all 32 places.
+ *   kv4_pool     uint8 [num_pages][num_kv_heads][TIDE_KV4_BLOCK_BYTES(d)], 16-byte aligned.  A
+ *                (page, KV head) block holds, one after the other,
+ *                  K codes  [4][16 slots][d/8 bytes]        entries (d/4) i .. of the slot
+ *                  V codes  [4][16][4 slots][d/32 bytes]    slots 4 i .., entries (d/16) j .. of each
+ *                  K scales [d/32 blocks][16 slots]         bytes s + 127; 255: NaN
+ *                  V scales [4][d/32 blocks][4 slots]
+ *                with the lower entry in a byte's lower half.
+ * Shapes, block tables, lengths, workspaces, streams and errors are those of the bf16 entry
+ * points; device buffers must be 16-byte aligned (TIDE_ERR_INVALID_ARG).
+ */
+#define TIDE_KV4_BLOCK_BYTES(head_dim) (17 * (head_dim))
+
+/*
+ * tide_kv_append into a 4-bit pool: the new tokens' K/V rows are rounded as above and stored in
+ * their slots; no other pool byte is written.
+ */
+TIDE_API int tide_kv4_append(const void* k_new, const void* v_new, void* kv4_pool,
+                    int64_t num_pages, const int32_t* block_table, int32_t bt_stride,
+                    int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
+                    const tide_dims* dims, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The reverse: k_out / v_out (bf16 [rows][Hkv][d], packed by extend_lens) receive the values that
+ * positions prefix_lens[b] .. prefix_lens[b] + extend_lens[b] - 1 of each task hold, for instance
+ * to append them to a bf16 pool again.  Rows of a page id out of range are zeros.
+ */
+TIDE_API int tide_kv4_unpack(const void* kv4_pool, int64_t num_pages, const int32_t* block_table,
+                    int32_t bt_stride, int32_t num_tasks, const int32_t* prefix_lens,
+                    const int32_t* extend_lens, const tide_dims* dims, void* k_out, void* v_out,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * tide_decode_attn over a 4-bit pool: the attention of the values that it holds, with the library's
+ * own split.  Workspace: TIDE_OP_KV4_DECODE.
+ */
+TIDE_API int tide_kv4_decode_attn(const void* q, const void* kv4_pool, int64_t num_pages,
+                         const int32_t* block_table, int32_t bt_stride, int32_t num_tasks,
+                         const int32_t* kv_lens, const tide_dims* dims, void* out, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * tide_decode_append_attn over a 4-bit pool: the result and the pool afterwards are those of
+ * tide_kv4_append of each task's newest token (position kv_lens[b] - 1) followed by
+ * tide_kv4_decode_attn; the token is attended as it is stored.
+ */
+TIDE_API int tide_kv4_decode_append_attn(const void* q, const void* k_new, const void* v_new,
+                                void* kv4_pool, int64_t num_pages, const int32_t* block_table,
+                                int32_t bt_stride, int32_t num_tasks, const int32_t* kv_lens,
+                                const tide_dims* dims, void* out, float* lse, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/*
+ * tide_extend_attn over a 4-bit pool (the new tokens appended before).  A call of a few tokens a task
+ * reads the codes themselves; a larger one unpacks its tasks' pages into the workspace and attends
+ * over those.  Workspace: TIDE_OP_KV4_EXTEND, up to 1 GiB of unpacked pages (one task's
+ * if that is more).
+ */
+TIDE_API int tide_kv4_extend_attn(const void* q, const void* kv4_pool, int64_t num_pages,
+                         const int32_t* block_table, int32_t bt_stride, int32_t num_tasks,
+                         const int32_t* prefix_lens, const int32_t* extend_lens,
+                         const tide_dims* dims, void* out, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* ---- eviction by accumulated attention weight ---------------------------------------------------
+ *
+ * A task whose context has to shrink keeps the positions that its queries attended to most.
+ * mass_pool: fp32 [num_pages][num_kv_heads][page_size], a sum per cached position and KV head that
+ * lies where the position's K/V lie (same page id and slot).
+ */
+
+/*
+ * Adds the attention weights of the new tokens' query rows to the sums of the keys they attended:
+ * for every KV head g and position p < prefix_lens[b] + extend_lens[b] of a task with
+ * extend_lens[b] > 0,
+ *   mass[p][g] = (p < counted_lens[b] ? mass[p][g] : 0)
+ *                + sum over new tokens j with prefix + j >= p, query heads h of g:
+ *                      exp(sm_scale * <q_jh, k_pg> - lse_jh)
+ *   q, lse        as the attention call took and returned them, packed by extend_lens
+ *   counted_lens  positions whose sums are carried on (at most prefix + extend); NULL: prefix_lens,
+ *                 so that the new tokens' own sums start at 0
+ * Tokens of which only the last w are to count: prefix + extend - w and w, with counted_lens = the
+ * prefix.  fp32 throughout, one writer per sum; two tasks must not map the same page (a sum of
+ * theirs is unspecified).  Workspace: TIDE_OP_ATTN_MASS.
+ */
+TIDE_API int tide_attn_mass(const void* q, const float* lse, const void* k_pool, int64_t num_pages,
+                   const int32_t* block_table, int32_t bt_stride, int32_t num_tasks,
+                   const int32_t* prefix_lens, const int32_t* extend_lens,
+                   const int32_t* counted_lens, const tide_dims* dims, float* mass_pool,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same over a 4-bit pool. */
+TIDE_API int tide_kv4_attn_mass(const void* q, const float* lse, const void* kv4_pool,
+                       int64_t num_pages, const int32_t* block_table, int32_t bt_stride,
+                       int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
+                       const int32_t* counted_lens, const tide_dims* dims, float* mass_pool,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cuts each task's context from kv_lens[b] to keep_lens[b] <= kv_lens[b] positions.  Every KV head
+ * keeps the last recent_lens[b] <= keep_lens[b] positions (NULL: none) and, of those before, the
+ * ones with the largest sums (equal sums: the earlier position; NaN counts as the least), and moves
+ * K, V and sums of what it keeps, in order, to positions 0 .. keep_lens[b] - 1.  The heads keep
+ * different positions: a key's position must already be part of its value (rotary K), and the
+ * task goes on with prefix keep_lens[b].
+ *   new_block_table  NULL: in place; pages from ceil(keep / 16) on are free afterwards, and no two
+ *                    tasks may share a page that one of them writes.  Else int32 [num_tasks]
+ *                    [new_bt_stride] (device): the pages that receive the kept positions; none of
+ *                    them may be listed by block_table in this call, and source pages may be shared.
+ *   kept             int32 [sum of keep_lens][Hkv] (device) or NULL: the kept positions, ascending
+ *                    per head, packed by keep_lens
+ * Slots past keep_lens[b] stay as they are.  A kept position whose own or new page id is out of
+ * range is not moved.  Workspace: TIDE_OP_KV_EVICT.
+ */
+TIDE_API int tide_kv_evict(void* k_pool, void* v_pool, float* mass_pool, int64_t num_pages,
+                  const int32_t* block_table, int32_t bt_stride, const int32_t* new_block_table,
+                  int32_t new_bt_stride, int32_t num_tasks, const int32_t* kv_lens,
+                  const int32_t* keep_lens, const int32_t* recent_lens, const tide_dims* dims,
+                  int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same over a 4-bit pool. */
+TIDE_API int tide_kv4_evict(void* kv4_pool, float* mass_pool, int64_t num_pages,
+                   const int32_t* block_table, int32_t bt_stride, const int32_t* new_block_table,
+                   int32_t new_bt_stride, int32_t num_tasks, const int32_t* kv_lens,
+                   const int32_t* keep_lens, const int32_t* recent_lens, const tide_dims* dims,
+                   int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable text for a status code (static storage, never NULL). */
 TIDE_API const char* tide_status_string(int status);

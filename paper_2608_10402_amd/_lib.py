@@ -26,6 +26,12 @@ TIDE_OP_KV_APPEND = 1
 TIDE_OP_EXTEND = 2
 TIDE_OP_DECODE = 3
 TIDE_OP_FULL_PREFILL = 4
+TIDE_OP_KV4_APPEND = 5
+TIDE_OP_KV4_UNPACK = 6
+TIDE_OP_KV4_DECODE = 7
+TIDE_OP_KV4_EXTEND = 8
+TIDE_OP_ATTN_MASS = 9
+TIDE_OP_KV_EVICT = 10
 
 # bytes of the static device scratch of tide_decode_attn_noalloc (TIDE_NOALLOC_SCRATCH_BYTES)
 NOALLOC_SCRATCH_BYTES = 64 << 20
@@ -33,6 +39,9 @@ NOALLOC_SCRATCH_BYTES = 64 << 20
 EXPORTED = ("tide_workspace_size", "tide_kv_append", "tide_extend_attn", "tide_decode_attn",
             "tide_full_prefill_attn", "tide_decode_attn_shared", "tide_workspace_size_shared",
             "tide_decode_append_attn", "tide_decode_attn_noalloc", "tide_extend_append_attn",
+            "tide_kv4_append", "tide_kv4_unpack", "tide_kv4_decode_attn",
+            "tide_kv4_decode_append_attn", "tide_kv4_extend_attn", "tide_attn_mass",
+            "tide_kv4_attn_mass", "tide_kv_evict", "tide_kv4_evict",
             "tide_plan_info_get", "tide_ctb_create", "tide_ctb_step", "tide_ctb_get_stats", "tide_ctb_destroy",
             "tide_status_string", "tide_shutdown")
 
@@ -94,6 +103,19 @@ def load(path: str = LIB_PATH):
                                             i32, vp, vp, vp, sz, vp]
     lib.tide_workspace_size_shared.argtypes = [i32, vp, i32, vp, vp, dims_p, i32,
                                                ctypes.POINTER(sz)]
+    lib.tide_kv4_append.argtypes = [vp, vp, vp, i64, vp, i32, i32, vp, vp, dims_p, vp, sz, vp]
+    lib.tide_kv4_unpack.argtypes = [vp, i64, vp, i32, i32, vp, vp, dims_p, vp, vp, vp, sz, vp]
+    lib.tide_kv4_decode_attn.argtypes = [vp, vp, i64, vp, i32, i32, vp, dims_p, vp, vp, vp, sz, vp]
+    lib.tide_kv4_decode_append_attn.argtypes = [vp, vp, vp, vp, i64, vp, i32, i32, vp, dims_p, vp, vp,
+                                                vp, sz, vp]
+    lib.tide_kv4_extend_attn.argtypes = [vp, vp, i64, vp, i32, i32, vp, vp, dims_p, vp, vp, vp, sz,
+                                         vp]
+    lib.tide_attn_mass.argtypes = [vp, vp, vp, i64, vp, i32, i32, vp, vp, vp, dims_p, vp, vp, sz, vp]
+    lib.tide_kv4_attn_mass.argtypes = lib.tide_attn_mass.argtypes
+    lib.tide_kv_evict.argtypes = [vp, vp, vp, i64, vp, i32, vp, i32, i32, vp, vp, vp, dims_p, vp, vp,
+                                  sz, vp]
+    lib.tide_kv4_evict.argtypes = [vp, vp, i64, vp, i32, vp, i32, i32, vp, vp, vp, dims_p, vp, vp,
+                                   sz, vp]
     lib.tide_plan_info_get.argtypes = [ctypes.c_int, i32, vp, vp, dims_p, i32,
                                        ctypes.POINTER(tide_plan_info)]
     lib.tide_ctb_create.argtypes = [vp, i32, vp, vp, i32, vp, vp, vp, vp, vp,
@@ -452,6 +474,230 @@ def tide_full_prefill_attn(q, k_pool, v_pool, block_table, seq_lens, dims: tide_
         s_p, ctypes.byref(dims), _dev(out, torch.bfloat16, "out"),
         _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n, _stream(stream)),
         "tide_full_prefill_attn")
+
+
+# ---- the 4-bit cache, attention mass, eviction ------------------------------------------------
+def kv4_block_bytes(head_dim: int) -> int:
+    """Bytes of one (page, kv head) block of a 4-bit pool (TIDE_KV4_BLOCK_BYTES)."""
+    return 17 * head_dim
+
+
+def _pool4_shape(kv4_pool, dims):
+    if kv4_pool.dim() != 3 or kv4_pool.shape[1:] != (dims.num_kv_heads,
+                                                     kv4_block_bytes(dims.head_dim)):
+        raise ValueError("kv4_pool must be [num_pages][Hkv][%d]" % kv4_block_bytes(dims.head_dim))
+    return kv4_pool.shape[0]
+
+
+def _per_task(lens, name, n):
+    """A host length array with one entry per task, or nothing."""
+    arr, ptr = _host(lens, name)
+    if arr is not None and arr.size != n:
+        raise ValueError("%s must have one entry per task" % name)
+    return arr, ptr
+
+
+def _pair(a, b, a_name, b_name):
+    a, a_p = _host(a, a_name)
+    b, b_p = _host(b, b_name)
+    if a is None or b is None or a.size != b.size:
+        raise ValueError("%s and %s must have one entry per task" % (a_name, b_name))
+    return a, a_p, b, b_p
+
+
+class _on_device:
+    """Makes the tensors' device the current one for a call (its stream, staging and launches)."""
+
+    def __init__(self, t):
+        self._to = t.get_device() if isinstance(t, torch.Tensor) and t.is_cuda else -1
+
+    def __enter__(self):
+        self._guard = None
+        if self._to >= 0 and self._to != torch.cuda.current_device():
+            self._guard = torch.cuda.device(self._to)
+            self._guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+def _mass_pool(mass, num_pages, dims):
+    if mass.shape != (num_pages, dims.num_kv_heads, dims.page_size):
+        raise ValueError("mass must be [num_pages][Hkv][page_size], got %s" % (tuple(mass.shape),))
+
+
+def tide_kv4_append(k_new, v_new, kv4_pool, block_table, prefix_lens, extend_lens, dims: tide_dims,
+                    workspace, stream=None) -> None:
+    num_pages = _pool4_shape(kv4_pool, dims)
+    p, p_p, e, e_p = _pair(prefix_lens, extend_lens, "prefix_lens", "extend_lens")
+    rows = _lens_total(e)
+    _rows(k_new, "k_new", rows, dims.num_kv_heads, dims.head_dim)
+    _rows(v_new, "v_new", rows, dims.num_kv_heads, dims.head_dim)
+    _block_table(block_table, int(p.size))
+    _same_device(k_new, v_new, kv4_pool, block_table, workspace)
+    ws, ws_n = _ws(workspace)
+    with _on_device(kv4_pool):
+        _check(load().tide_kv4_append(
+            _dev(k_new, torch.bfloat16, "k_new"), _dev(v_new, torch.bfloat16, "v_new"),
+            _dev(kv4_pool, torch.uint8, "kv4_pool"), num_pages,
+            _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(p.size),
+            p_p, e_p, ctypes.byref(dims), ws, ws_n, _stream(stream)), "tide_kv4_append")
+
+
+def tide_kv4_unpack(kv4_pool, block_table, prefix_lens, extend_lens, dims: tide_dims, k_out, v_out,
+                    workspace, stream=None) -> None:
+    num_pages = _pool4_shape(kv4_pool, dims)
+    p, p_p, e, e_p = _pair(prefix_lens, extend_lens, "prefix_lens", "extend_lens")
+    rows = _lens_total(e)
+    _rows(k_out, "k_out", rows, dims.num_kv_heads, dims.head_dim)
+    _rows(v_out, "v_out", rows, dims.num_kv_heads, dims.head_dim)
+    _block_table(block_table, int(p.size))
+    _same_device(k_out, v_out, kv4_pool, block_table, workspace)
+    ws, ws_n = _ws(workspace)
+    with _on_device(kv4_pool):
+        _check(load().tide_kv4_unpack(
+            _dev(kv4_pool, torch.uint8, "kv4_pool"), num_pages,
+            _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(p.size),
+            p_p, e_p, ctypes.byref(dims), _dev(k_out, torch.bfloat16, "k_out"),
+            _dev(v_out, torch.bfloat16, "v_out"), ws, ws_n, _stream(stream)), "tide_kv4_unpack")
+
+
+def tide_kv4_decode_attn(q, kv4_pool, block_table, kv_lens, dims: tide_dims, out, lse=None,
+                         workspace=None, stream=None) -> None:
+    num_pages = _pool4_shape(kv4_pool, dims)
+    kv, kv_p = _host(kv_lens, "kv_lens")
+    _decode_checks(q, out, lse, block_table, kv, dims, kv4_pool, workspace)
+    ws, ws_n = _ws(workspace)
+    with _on_device(kv4_pool):
+        _check(load().tide_kv4_decode_attn(
+            _dev(q, torch.bfloat16, "q"), _dev(kv4_pool, torch.uint8, "kv4_pool"), num_pages,
+            _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(kv.size),
+            kv_p, ctypes.byref(dims), _dev(out, torch.bfloat16, "out"),
+            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n, _stream(stream)),
+            "tide_kv4_decode_attn")
+
+
+def tide_kv4_decode_append_attn(q, k_new, v_new, kv4_pool, block_table, kv_lens, dims: tide_dims,
+                                out, lse=None, workspace=None, stream=None) -> None:
+    num_pages = _pool4_shape(kv4_pool, dims)
+    kv, kv_p = _host(kv_lens, "kv_lens")
+    _decode_checks(q, out, lse, block_table, kv, dims, kv4_pool, k_new, v_new, workspace)
+    _rows(k_new, "k_new", int(kv.size), dims.num_kv_heads, dims.head_dim)
+    _rows(v_new, "v_new", int(kv.size), dims.num_kv_heads, dims.head_dim)
+    ws, ws_n = _ws(workspace)
+    with _on_device(kv4_pool):
+        _check(load().tide_kv4_decode_append_attn(
+            _dev(q, torch.bfloat16, "q"), _dev(k_new, torch.bfloat16, "k_new"),
+            _dev(v_new, torch.bfloat16, "v_new"), _dev(kv4_pool, torch.uint8, "kv4_pool"),
+            num_pages, _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]),
+            int(kv.size), kv_p, ctypes.byref(dims), _dev(out, torch.bfloat16, "out"),
+            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n, _stream(stream)),
+            "tide_kv4_decode_append_attn")
+
+
+def tide_kv4_extend_attn(q, kv4_pool, block_table, prefix_lens, extend_lens, dims: tide_dims, out,
+                         lse=None, workspace=None, stream=None) -> None:
+    num_pages = _pool4_shape(kv4_pool, dims)
+    p, p_p, e, e_p = _pair(prefix_lens, extend_lens, "prefix_lens", "extend_lens")
+    rows = _lens_total(e)
+    _rows(q, "q", rows, dims.num_q_heads, dims.head_dim)
+    _rows(out, "out", rows, dims.num_q_heads, dims.head_dim)
+    _lse(lse, rows, dims.num_q_heads)
+    _block_table(block_table, int(p.size))
+    _same_device(q, kv4_pool, block_table, out, lse, workspace)
+    ws, ws_n = _ws(workspace)
+    with _on_device(kv4_pool):
+        _check(load().tide_kv4_extend_attn(
+            _dev(q, torch.bfloat16, "q"), _dev(kv4_pool, torch.uint8, "kv4_pool"), num_pages,
+            _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(p.size),
+            p_p, e_p, ctypes.byref(dims), _dev(out, torch.bfloat16, "out"),
+            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n, _stream(stream)),
+            "tide_kv4_extend_attn")
+
+
+def _attn_mass(name, q, lse, pool, pool_type, num_pages, block_table, prefix_lens, extend_lens,
+               dims, mass, counted_lens, workspace, stream):
+    p, p_p, e, e_p = _pair(prefix_lens, extend_lens, "prefix_lens", "extend_lens")
+    counted, c_p = _per_task(counted_lens, "counted_lens", int(p.size))  # (held for the call)
+    rows = _lens_total(e)
+    _rows(q, "q", rows, dims.num_q_heads, dims.head_dim)
+    _lse(lse, rows, dims.num_q_heads)
+    _mass_pool(mass, num_pages, dims)
+    _block_table(block_table, int(p.size))
+    _same_device(q, lse, pool, block_table, mass, workspace)
+    ws, ws_n = _ws(workspace)
+    with _on_device(pool):
+        _check(getattr(load(), name)(
+            _dev(q, torch.bfloat16, "q"), _dev(lse, torch.float32, "lse"),
+            _dev(pool, pool_type, "pool"), num_pages,
+            _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(p.size),
+            p_p, e_p, c_p, ctypes.byref(dims), _dev(mass, torch.float32, "mass"), ws, ws_n,
+            _stream(stream)), name)
+
+
+def tide_attn_mass(q, lse, k_pool, block_table, prefix_lens, extend_lens, dims: tide_dims, mass,
+                   counted_lens=None, workspace=None, stream=None) -> None:
+    _attn_mass("tide_attn_mass", q, lse, k_pool, torch.bfloat16, _pool_shape(k_pool, k_pool, dims),
+               block_table, prefix_lens, extend_lens, dims, mass, counted_lens, workspace, stream)
+
+
+def tide_kv4_attn_mass(q, lse, kv4_pool, block_table, prefix_lens, extend_lens, dims: tide_dims,
+                       mass, counted_lens=None, workspace=None, stream=None) -> None:
+    _attn_mass("tide_kv4_attn_mass", q, lse, kv4_pool, torch.uint8, _pool4_shape(kv4_pool, dims),
+               block_table, prefix_lens, extend_lens, dims, mass, counted_lens, workspace, stream)
+
+
+def _evict_lens(mass, num_pages, block_table, new_block_table, kv_lens, keep_lens, recent_lens, kept,
+                dims):
+    n, n_p, k, k_p = _pair(kv_lens, keep_lens, "kv_lens", "keep_lens")
+    r, r_p = _per_task(recent_lens, "recent_lens", int(n.size))
+    _mass_pool(mass, num_pages, dims)
+    _block_table(block_table, int(n.size))
+    new, new_p, stride = new_block_table, None, 0
+    if new is not None:
+        stride = _block_table(new, int(n.size))
+        new_p = _dev(new, torch.int32, "new_block_table")
+    total = _lens_total(k)
+    if kept is not None and total is not None and kept.shape != (total, dims.num_kv_heads):
+        raise ValueError("kept must have shape (%d, %d), got %s"
+                         % (total, dims.num_kv_heads, tuple(kept.shape)))
+    return (n, k, r), n_p, k_p, r_p, new_p, int(stride)
+
+
+def tide_kv_evict(k_pool, v_pool, mass, block_table, kv_lens, keep_lens, dims: tide_dims,
+                  recent_lens=None, new_block_table=None, kept=None, workspace=None,
+                  stream=None) -> None:
+    num_pages = _pool_shape(k_pool, v_pool, dims)
+    hold, n_p, k_p, r_p, new_p, stride = _evict_lens(mass, num_pages, block_table, new_block_table,
+                                                     kv_lens, keep_lens, recent_lens, kept, dims)
+    _same_device(k_pool, v_pool, mass, block_table, new_block_table, kept, workspace)
+    ws, ws_n = _ws(workspace)
+    with _on_device(k_pool):
+        _check(load().tide_kv_evict(
+            _dev(k_pool, torch.bfloat16, "k_pool"), _dev(v_pool, torch.bfloat16, "v_pool"),
+            _dev(mass, torch.float32, "mass"), num_pages,
+            _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), new_p, stride,
+            int(hold[0].size), n_p, k_p, r_p, ctypes.byref(dims),
+            _dev(kept, torch.int32, "kept", nullable=True), ws, ws_n, _stream(stream)),
+            "tide_kv_evict")
+
+
+def tide_kv4_evict(kv4_pool, mass, block_table, kv_lens, keep_lens, dims: tide_dims,
+                   recent_lens=None, new_block_table=None, kept=None, workspace=None,
+                   stream=None) -> None:
+    num_pages = _pool4_shape(kv4_pool, dims)
+    hold, n_p, k_p, r_p, new_p, stride = _evict_lens(mass, num_pages, block_table, new_block_table,
+                                                     kv_lens, keep_lens, recent_lens, kept, dims)
+    _same_device(kv4_pool, mass, block_table, new_block_table, kept, workspace)
+    ws, ws_n = _ws(workspace)
+    with _on_device(kv4_pool):
+        _check(load().tide_kv4_evict(
+            _dev(kv4_pool, torch.uint8, "kv4_pool"), _dev(mass, torch.float32, "mass"), num_pages,
+            _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), new_p, stride,
+            int(hold[0].size), n_p, k_p, r_p, ctypes.byref(dims),
+            _dev(kept, torch.int32, "kept", nullable=True), ws, ws_n, _stream(stream)),
+            "tide_kv4_evict")
 
 
 def tide_shutdown() -> None:

@@ -22,7 +22,8 @@ LIB_PATH = os.path.join(PKG, "libtide.so")
 
 HIP_SOURCES = ["tide_api.hip", "attn_extend.hip", "attn_extend_append.hip", "attn_decode.hip",
                "attn_decode_stream.hip",
-               "kv_append.hip"]
+               "kv_append.hip", "cache_api.hip", "kv4_store.hip", "kv4_decode.hip", "attn_mass.hip",
+               "kv_evict.hip"]
 CXX_SOURCES = ["plan.cpp", "ctb.cpp"]
 ARCH = "gfx950"
 

@@ -24,4 +24,14 @@ int append_waves();
 // Workgroups of the append kernel per work item.
 int append_groups(int32_t num_kv_heads);
 
+// The 4-bit cache: append (k_new set) or unpack, whole pages for an extend, attention of units.
+hipError_t launch_kv4_store(const Kv4StoreArgs& a, hipStream_t stream);
+hipError_t launch_kv4_stage(const Kv4StageArgs& a, hipStream_t stream);
+hipError_t launch_kv4_decode(const Kv4AttnArgs& a, int head_dim, hipStream_t stream);
+// Workgroups of the store kernel per work item.
+int kv4_store_groups(int32_t num_kv_heads);
+// Attention mass over a bf16 K pool or the 4-bit pool, and eviction from either.
+hipError_t launch_attn_mass(const MassArgs& a, int head_dim, bool kv4, hipStream_t stream);
+hipError_t launch_evict(const EvictArgs& a, int head_dim, bool kv4, hipStream_t stream);
+
 }  // namespace tide

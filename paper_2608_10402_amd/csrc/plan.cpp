@@ -995,4 +995,274 @@ int make_plan_shared(int32_t num_tasks, const int32_t* kv_lens, int32_t num_grou
   return TIDE_OK;
 }
 
+// ---- the 4-bit cache, attention mass, eviction ----------------------------------------------
+
+namespace {
+
+constexpr int64_t kKv4WaveSlots = 2048;
+constexpr int64_t kKv4StageBytes = (int64_t)1 << 30;
+constexpr int32_t kKv4StagePages = 16;  // of a staging item
+constexpr int32_t kKv4DirectTokens = 16;
+
+// Appends `n` records to a plan's blob region at `off` (grown to its end) and returns the end.
+template <class T>
+size_t put(std::vector<uint8_t>* blob, size_t off, const std::vector<T>& v) {
+  const size_t bytes = v.size() * sizeof(T);
+  if (blob->size() < off + bytes) blob->resize(off + bytes);
+  if (bytes) memcpy(blob->data() + off, v.data(), bytes);
+  return off + bytes;
+}
+
+}  // namespace
+
+int make_plan_kv4_units(int op, int32_t num_tasks, const int32_t* lens_a, const int32_t* lens_b,
+                        const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan) {
+  if (!plan || num_tasks < 0 || (num_tasks > 0 && !lens_a)) return TIDE_ERR_INVALID_ARG;
+  if (op != TIDE_OP_KV4_DECODE && op != TIDE_OP_KV4_EXTEND) return TIDE_ERR_INVALID_ARG;
+  if (num_tasks > 0 && op == TIDE_OP_KV4_EXTEND && !lens_b) return TIDE_ERR_INVALID_ARG;
+  int rc = check_dims(&dims);
+  if (rc != TIDE_OK) return rc;
+  const int32_t hkv = dims.num_kv_heads, group = dims.num_q_heads / hkv;
+  const int32_t most = op == TIDE_OP_KV4_DECODE ? 1 : kKv4Cols / group;  // tokens of a unit
+  std::vector<TaskDesc> units;
+  int64_t total = 0, longest = 0, rows = 0;
+  int32_t widest = 1;
+  for (int32_t b = 0; b < num_tasks; ++b) {
+    int32_t p = 0, e = 0;
+    rc = task_lengths(op == TIDE_OP_KV4_DECODE ? TIDE_OP_DECODE : TIDE_OP_EXTEND, b, lens_a, lens_b, &p, &e);
+    if (rc != TIDE_OK) return rc;
+    if (rows + e > INT32_MAX) return TIDE_ERR_INVALID_ARG;
+    if (bt_stride >= 0 && ceil_div((int64_t)p + e, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
+    for (int32_t t = 0; t < e; t += most) {
+      const int32_t n = std::min(most, e - t);
+      units.push_back(TaskDesc{(int32_t)rows + t, p + t, n, b});
+      const int64_t st = ceil_div((int64_t)p + t + n, kDecodeStep);
+      total += st;
+      longest = std::max(longest, st);
+      widest = std::max(widest, n);
+    }
+    rows += e;
+  }
+  if (units.size() > (size_t)INT32_MAX / kMaxGroup) return TIDE_ERR_INVALID_ARG;
+  *plan = Plan();
+  plan->op = op;
+  plan->num_tasks = (int32_t)units.size();
+  plan->total_rows = (int32_t)rows;
+  plan->tokens_per_item = widest;
+  if (units.empty()) {
+    plan->total_bytes = plan->upload_bytes = sizeof(WsHeader);
+    return TIDE_OK;
+  }
+  int64_t steps = ceil_div(total, std::max<int64_t>(1, kKv4WaveSlots / hkv));
+  while (kStreamMergeSteps * (steps + 1) * (steps + 1) <= longest) ++steps;
+  if (steps > INT32_MAX / kDecodeStep) return TIDE_ERR_INVALID_ARG;
+  plan->stream = true;
+  plan->steps = (int32_t)steps;
+  plan->num_runs = (int32_t)ceil_div(total, steps);
+  plan->last_steps = (int32_t)(total - (int64_t)(plan->num_runs - 1) * steps);
+  if ((int64_t)plan->num_runs * hkv > INT32_MAX / 4) return TIDE_ERR_INVALID_ARG;
+  plan->num_items = plan->num_runs * hkv;
+
+  size_t off = sizeof(WsHeader);
+  plan->tasks_off = off;
+  off = align_up(off + units.size() * sizeof(TaskDesc), kWsAlign);
+  plan->items_off = off;
+  off = align_up(off + (size_t)plan->num_runs * sizeof(StreamItem), kWsAlign);
+  const StreamSlots per_head = {plan->num_runs, plan->num_tasks, kv4_waves(plan->num_items)};
+  plan->tickets_off = off;  // the parts' flags
+  off = align_up(off + (size_t)per_head.count() * hkv * sizeof(uint64_t), kWsAlign);
+  plan->upload_bytes = off;
+  const size_t slots = (size_t)per_head.count() * hkv * widest * group;
+  plan->part_o_off = off;
+  off = align_up(off + slots * dims.head_dim * sizeof(float), kWsAlign);
+  plan->part_ml_off = off;
+  off = align_up(off + slots * 4 * sizeof(float), kWsAlign);
+  plan->total_bytes = off;
+  if (!build_blob) return TIDE_OK;
+  plan->blob.assign(plan->upload_bytes, 0);
+  memcpy(plan->blob.data() + plan->tasks_off, units.data(), units.size() * sizeof(TaskDesc));
+  StreamItem* items = reinterpret_cast<StreamItem*>(plan->blob.data() + plan->items_off);
+  int64_t at = 0, run = 0;  // first step of the unit, next run to place
+  for (size_t u = 0; u < units.size(); ++u) {
+    const int32_t kv_len = units[u].prefix + units[u].extend;
+    const int64_t end = at + ceil_div(kv_len, kDecodeStep);
+    for (; run * steps < end; ++run)
+      items[run] = StreamItem{(int32_t)u, (int32_t)(run * steps - at), kv_len, 0};
+    at = end;
+  }
+  return TIDE_OK;
+}
+
+int make_plan_kv4_extend(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
+                         const tide_dims& dims, int32_t bt_stride, bool build_blob, Kv4ExtendPlan* plan) {
+  if (!plan || num_tasks < 0 || (num_tasks > 0 && (!prefix_lens || !extend_lens))) return TIDE_ERR_INVALID_ARG;
+  int rc = check_dims(&dims);
+  if (rc != TIDE_OK) return rc;
+  *plan = Kv4ExtendPlan();
+  int32_t longest = 0;
+  int64_t rows = 0;
+  for (int32_t b = 0; b < num_tasks; ++b) {
+    int32_t p = 0, e = 0;
+    rc = task_lengths(TIDE_OP_EXTEND, b, prefix_lens, extend_lens, &p, &e);
+    if (rc != TIDE_OK) return rc;
+    rows += e;
+    if (rows > INT32_MAX) return TIDE_ERR_INVALID_ARG;
+    if (bt_stride >= 0 && ceil_div((int64_t)p + e, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
+    longest = std::max(longest, e);
+  }
+  if (longest <= kKv4DirectTokens) {
+    plan->by_units = true;
+    rc = make_plan_kv4_units(TIDE_OP_KV4_EXTEND, num_tasks, prefix_lens, extend_lens, dims, bt_stride, build_blob,
+                             &plan->units);
+    plan->total_bytes = plan->units.total_bytes;
+    return rc;
+  }
+  const int64_t page_bytes = (int64_t)dims.num_kv_heads * kPage * dims.head_dim * 2 * 2;  // K and V
+  auto pages_of = [&](int32_t b) {
+    return extend_lens[b] ? ceil_div((int64_t)prefix_lens[b] + extend_lens[b], kPage) : 0;
+  };
+  size_t stage_bytes = 0, extend_bytes = 0, table_bytes = 0;
+  int64_t pool_pages = 0, row0 = 0;
+  for (int32_t b = 0; b < num_tasks;) {
+    plan->rounds.emplace_back();
+    Kv4Round& r = plan->rounds.back();
+    r.first = b;
+    r.row0 = row0;
+    int64_t round_rows = 0;
+    while (b < num_tasks && (r.pages == 0 || (r.pages + pages_of(b)) * page_bytes <= kKv4StageBytes)) {
+      r.pages += pages_of(b);
+      r.stride = std::max(r.stride, (int32_t)pages_of(b));
+      round_rows += extend_lens[b++];
+    }
+    r.tasks = b - r.first;
+    row0 += round_rows;
+    if (round_rows == 0) {
+      plan->rounds.pop_back();
+      continue;
+    }
+    if (r.pages > INT32_MAX) return TIDE_ERR_INVALID_ARG;
+    rc = make_plan(TIDE_OP_EXTEND, r.tasks, prefix_lens + r.first, extend_lens + r.first, dims, 0, -1, build_blob,
+                   &r.extend);
+    if (rc != TIDE_OK) return rc;
+    std::vector<Kv4StageItem> items;
+    int64_t to = 0;
+    for (int32_t i = 0; i < r.tasks; ++i) {
+      const int64_t n = pages_of(r.first + i);
+      for (int64_t lp = 0; lp < n; lp += kKv4StagePages) {
+        const int32_t k = (int32_t)std::min<int64_t>(kKv4StagePages, n - lp);
+        items.push_back(Kv4StageItem{r.first + i, (int32_t)lp, k, (int32_t)to, i, {0, 0, 0}});
+        to += k;
+      }
+    }
+    if (items.size() > (size_t)INT32_MAX) return TIDE_ERR_INVALID_ARG;
+    Plan& st = r.stage;
+    st.op = TIDE_OP_KV4_EXTEND;
+    st.num_tasks = r.tasks;
+    st.num_items = (int32_t)items.size();
+    st.items_off = sizeof(WsHeader);
+    st.upload_bytes = st.total_bytes = align_up(st.items_off + items.size() * sizeof(Kv4StageItem), kWsAlign);
+    if (build_blob) {
+      put(&st.blob, st.items_off, items);
+      st.blob.resize(st.upload_bytes, 0);
+    }
+    stage_bytes = std::max(stage_bytes, st.total_bytes);
+    extend_bytes = std::max(extend_bytes, r.extend.total_bytes);
+    table_bytes = std::max(table_bytes, (size_t)r.tasks * r.stride * sizeof(int32_t));
+    pool_pages = std::max(pool_pages, r.pages);
+  }
+  size_t off = 0;
+  plan->stage_off = off;
+  off = align_up(off + std::max(stage_bytes, sizeof(WsHeader)), kWsAlign);
+  plan->extend_off = off;
+  off = align_up(off + extend_bytes, kWsAlign);
+  plan->table_off = off;
+  off = align_up(off + table_bytes, kWsAlign);
+  plan->pool_off = off;
+  plan->total_bytes = off + (size_t)(pool_pages * page_bytes);
+  return TIDE_OK;
+}
+
+int make_plan_mass(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
+                   const int32_t* counted, const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan) {
+  if (!plan || num_tasks < 0 || (num_tasks > 0 && (!prefix_lens || !extend_lens))) return TIDE_ERR_INVALID_ARG;
+  int rc = check_dims(&dims);
+  if (rc != TIDE_OK) return rc;
+  *plan = Plan();
+  plan->op = TIDE_OP_ATTN_MASS;
+  plan->num_tasks = num_tasks;
+  std::vector<TaskDesc> tasks((size_t)num_tasks);
+  std::vector<MassItem> items;
+  int64_t rows = 0, n_items = 0;
+  for (int32_t b = 0; b < num_tasks; ++b) {
+    int32_t p = 0, e = 0;
+    rc = task_lengths(TIDE_OP_EXTEND, b, prefix_lens, extend_lens, &p, &e);
+    if (rc != TIDE_OK) return rc;
+    const int32_t c = counted ? counted[b] : p;
+    if (c < 0 || c > p + e) return TIDE_ERR_INVALID_ARG;
+    tasks[b] = TaskDesc{(int32_t)rows, p, e, c};
+    rows += e;
+    if (rows > INT32_MAX) return TIDE_ERR_INVALID_ARG;
+    if (bt_stride >= 0 && ceil_div((int64_t)p + e, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
+    if (e == 0) continue;
+    n_items += ceil_div((int64_t)p + e, kMassKeys);
+    if (build_blob)
+      for (int64_t k = 0; k < (int64_t)p + e; k += kMassKeys) items.push_back(MassItem{b, (int32_t)k});
+  }
+  if (n_items * dims.num_kv_heads > INT32_MAX / 4) return TIDE_ERR_INVALID_ARG;
+  plan->num_items = (int32_t)n_items;
+  plan->total_rows = (int32_t)rows;
+  size_t off = sizeof(WsHeader);
+  plan->tasks_off = off;
+  off = align_up(off + tasks.size() * sizeof(TaskDesc), kWsAlign);
+  plan->items_off = off;
+  off = align_up(off + (size_t)n_items * sizeof(MassItem), kWsAlign);
+  plan->upload_bytes = plan->total_bytes = off;
+  if (!build_blob) return TIDE_OK;
+  put(&plan->blob, plan->tasks_off, tasks);
+  put(&plan->blob, plan->items_off, items);
+  plan->blob.resize(plan->upload_bytes, 0);
+  return TIDE_OK;
+}
+
+int make_plan_evict(int32_t num_tasks, const int32_t* kv_lens, const int32_t* keep_lens, const int32_t* recent,
+                    const tide_dims& dims, int32_t bt_stride, int32_t new_stride, bool build_blob, Plan* plan) {
+  if (!plan || num_tasks < 0 || (num_tasks > 0 && (!kv_lens || !keep_lens))) return TIDE_ERR_INVALID_ARG;
+  int rc = check_dims(&dims);
+  if (rc != TIDE_OK) return rc;
+  *plan = Plan();
+  plan->op = TIDE_OP_KV_EVICT;
+  std::vector<EvictTask> tasks;
+  int64_t kept = 0;
+  int32_t longest = 0;
+  for (int32_t b = 0; b < num_tasks; ++b) {
+    const int32_t n = kv_lens[b], k = keep_lens[b], r = recent ? recent[b] : 0;
+    if (n < 0 || k < 0 || k > n || r < 0 || r > k) return TIDE_ERR_INVALID_ARG;
+    if (bt_stride >= 0 && ceil_div(n, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
+    if (new_stride >= 0 && ceil_div(k, kPage) > new_stride) return TIDE_ERR_CAPACITY;
+    if (k > 0) tasks.push_back(EvictTask{b, n, k, r, (int32_t)kept, {0, 0, 0}});
+    kept += k;
+    if (kept > INT32_MAX) return TIDE_ERR_INVALID_ARG;
+    longest = std::max(longest, k);
+  }
+  if ((int64_t)tasks.size() * dims.num_kv_heads > INT32_MAX / 4) return TIDE_ERR_INVALID_ARG;
+  plan->num_tasks = (int32_t)tasks.size();
+  plan->num_items = plan->num_tasks;
+  plan->total_rows = (int32_t)kept;
+  plan->chunk = longest;
+  size_t off = sizeof(WsHeader);
+  plan->tasks_off = off;
+  off = align_up(off + tasks.size() * sizeof(EvictTask), kWsAlign);
+  plan->upload_bytes = off;
+  const size_t n = (size_t)kept * dims.num_kv_heads;
+  plan->items_off = off;
+  off = align_up(off + n * sizeof(EvictIndex), kWsAlign);
+  plan->part_ml_off = off;
+  off = align_up(off + n * sizeof(float), kWsAlign);
+  plan->total_bytes = off;
+  if (!build_blob) return TIDE_OK;
+  put(&plan->blob, plan->tasks_off, tasks);
+  plan->blob.resize(plan->upload_bytes, 0);
+  return TIDE_OK;
+}
+
 }  // namespace tide

@@ -85,6 +85,44 @@ int make_plan_shared(int32_t num_tasks, const int32_t* kv_lens, int32_t num_grou
                      const tide_dims& dims, int32_t num_splits, int32_t bt_stride,
                      bool build_blob, Plan* plan);
 
+// ---- the 4-bit cache, attention mass, eviction ----------------------------------------------
+// Runs of steps over units of up to kKv4Cols / G query tokens each (Kv4AttnArgs).  lens_a, lens_b as
+// TIDE_OP_KV4_DECODE or TIDE_OP_KV4_EXTEND take them.
+int make_plan_kv4_units(int op, int32_t num_tasks, const int32_t* lens_a, const int32_t* lens_b,
+                        const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan);
+
+// An extend over the 4-bit cache: by units, or by rounds of consecutive tasks whose pages are
+// unpacked into a staging area of the workspace that the bf16 extend kernel reads.
+struct Kv4Round {
+  int32_t first = 0, tasks = 0;  // consecutive tasks
+  int64_t row0 = 0;              // the first one's packed row
+  Plan stage;                    // Kv4StageItems
+  Plan extend;
+  int32_t stride = 0;            // of the staging block table
+  int64_t pages = 0;             // staged
+};
+
+struct Kv4ExtendPlan {
+  bool by_units = false;
+  Plan units;
+  std::vector<Kv4Round> rounds;
+  // byte offsets of a round's parts (the rounds follow each other in the same bytes)
+  size_t stage_off = 0, extend_off = 0, table_off = 0, pool_off = 0;
+  size_t total_bytes = 0;
+};
+
+int make_plan_kv4_extend(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
+                         const tide_dims& dims, int32_t bt_stride, bool build_blob, Kv4ExtendPlan* plan);
+
+// Attention mass: MassItems.  counted: positions per task whose sums are carried on (null: prefix).
+int make_plan_mass(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
+                   const int32_t* counted, const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan);
+
+// Eviction: EvictTasks (at tasks_off); the index at items_off, its sums at part_ml_off.  recent may be
+// null (0 everywhere); new_stride < 0: the new pages' capacity is not checked.
+int make_plan_evict(int32_t num_tasks, const int32_t* kv_lens, const int32_t* keep_lens, const int32_t* recent,
+                    const tide_dims& dims, int32_t bt_stride, int32_t new_stride, bool build_blob, Plan* plan);
+
 // Waves per workgroup of the extend kernel for a head size and GQA group.
 int32_t extend_waves(int32_t head_dim, int32_t group);
 

@@ -19,17 +19,10 @@
 
 #include "kernels.h"
 #include "plan.h"
+#include "staging.h"
 #include "tide.h"
 
 namespace tide {
-namespace {
-
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-
-constexpr int kStagingSlots = 16;
-// Slots start large and grow by powers of two, so that steady-state calls never
-// reallocate: freeing and allocating pinned memory is slow and can stall the device.
-constexpr size_t kStagingMin = 2u << 20;
 
 // Pinned, device-mapped host buffers the work lists are staged in.  The call's own kernel
 // reads a slot in place, or a kernel on the caller's stream copies it into the workspace (no
@@ -48,6 +41,15 @@ struct StagingSlot {
   uint32_t nblocks = 0;       // workgroups of the last reader
   bool pending = false;
 };
+
+namespace {
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kStagingSlots = 16;
+// Slots start large and grow by powers of two, so that steady-state calls never
+// reallocate: freeing and allocating pinned memory is slow and can stall the device.
+constexpr size_t kStagingMin = 2u << 20;
 
 constexpr int kCopyBytesPerBlock = 256 * 16;
 
@@ -171,25 +173,6 @@ bool debug_checks() {
   return e && e[0] == '1';
 }
 
-// Where a call's kernel finds its plan.
-struct Staged {
-  const uint8_t* plan = nullptr;  // the workspace, or a staging slot
-  PlanReads reads = {nullptr, 0};
-  StagingSlot* slot = nullptr;    // set with reads.done
-  // the ring's, held with a slot until its reader is launched: until then another call that
-  // came round to the slot would wait for flags that no kernel is there to set
-  std::unique_lock<std::mutex> lock;
-};
-
-// A plan that at most this many workgroups read, once each, is read where it was staged: a
-// record costs each a read of host memory (about 2 us), which is less than the copy kernel,
-// its launch and the gap behind it (3-5 us on the GPU and 3 on the host): a four-task decode
-// step went from 16.0 to 13.5 us, the smallest append + extend from 31 to 25.  Each workgroup
-// pays for its own read, so the gain ends where an extend's workgroups come in rounds of the
-// CUs: copied and in place, us a call (28 / 4 heads, d = 128), extends of 64 workgroups 18.5 and
-// 16.5, 256 23.5 and 20.9, 512 38.3 and 38.9, 1,024 69.5 and 79, 2,000 134 and 145; appends of 512
-// 20.8 and 18.3, 1,024 21.4 and 18.4; decodes (up to 256 workgroups at 4 kv heads) 2 us less.
-constexpr uint32_t kInPlaceGroups = 512;
 static_assert(kStagingMin / kCopyBytesPerBlock >= kInPlaceGroups, "every slot has a flag for each");
 
 bool capturing(hipStream_t stream) {
@@ -201,9 +184,8 @@ bool capturing(hipStream_t stream) {
   return st != hipStreamCaptureStatusNone;
 }
 
-// Stages the plan.  readers: the workgroups of the one kernel that reads it, if it may be read
-// in place (0: not).  Under debug checks the kernel needs the zeroed header, which keeps the
-// copy into the workspace; under capture no staging slot is used.
+}  // namespace
+
 int upload(const Plan& plan, void* workspace, hipStream_t stream, uint32_t readers, Staged* out) {
   if (capturing(stream)) {
     out->plan = static_cast<const uint8_t*>(workspace);
@@ -283,18 +265,6 @@ int finish(hipError_t launch_status, Staged& st, void* workspace, hipStream_t st
   return (flags & 1) ? TIDE_ERR_PAGE_RANGE : TIDE_OK;
 }
 
-template <class T>
-const T* at(const void* ws, size_t off) {
-  return reinterpret_cast<const T*>(static_cast<const uint8_t*>(ws) + off);
-}
-
-template <class T>
-T* at_mut(void* ws, size_t off) {
-  return reinterpret_cast<T*>(static_cast<uint8_t*>(ws) + off);
-}
-
-// A number no other call of the process has, and no chance contents of a workspace: the count
-// starts at a random 64-bit number.
 uint64_t next_call() {
   static std::atomic<uint64_t> count([] {
     std::random_device r;
@@ -305,6 +275,42 @@ uint64_t next_call() {
   while (c == 0);  // what a copied plan zeroes the flags to
   return c;
 }
+
+int run_extend_plan(const Plan& plan, const void* q, const void* k_pool, const void* v_pool, int64_t num_pages,
+                    const int32_t* block_table, int32_t bt_stride, const tide_dims& dims, void* out, float* lse,
+                    void* workspace, hipStream_t s, const void* k_new, const void* v_new) {
+  Staged st;
+  const int rc = upload(plan, workspace, s, plan.split ? 0 : (uint32_t)plan.num_items, &st);
+  if (rc != TIDE_OK) return rc;
+  ExtendArgs a;
+  a.reads = st.reads;
+  a.k_new = static_cast<const uint16_t*>(k_new);
+  a.v_new = static_cast<const uint16_t*>(v_new);
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_pool = static_cast<const uint16_t*>(k_pool);
+  a.v_pool = static_cast<const uint16_t*>(v_pool);
+  a.block_table = block_table;
+  a.num_pages = num_pages;
+  a.bt_stride = bt_stride;
+  a.num_q_heads = dims.num_q_heads;
+  a.num_kv_heads = dims.num_kv_heads;
+  a.group = dims.num_q_heads / dims.num_kv_heads;
+  a.scale_log2 = dims.sm_scale * 1.44269504088896340736f;
+  a.num_items = plan.num_items;
+  a.tasks = at<TaskDesc>(st.plan, plan.tasks_off);
+  a.items = plan.split ? nullptr : at<ExtendItem>(st.plan, plan.items_off);
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.error_flags = at_mut<int32_t>(workspace, 0);
+  a.chunk_items = plan.split ? at<ExtendChunkItem>(workspace, plan.items_off) : nullptr;
+  a.merge_rows = plan.split ? at<MergeRow>(workspace, plan.merge_rows_off) : nullptr;
+  a.part_o = plan.split ? at_mut<float>(workspace, plan.part_o_off) : nullptr;
+  a.part_ml = plan.split ? at_mut<float>(workspace, plan.part_ml_off) : nullptr;
+  a.total_rows = plan.total_rows;
+  return finish(launch_extend(a, dims.head_dim, plan.waves, s), st, workspace, s);
+}
+
+namespace {
 
 // Shared path of tide_extend_attn and tide_full_prefill_attn.
 // With k_new / v_new (tide_extend_append_attn) the new tokens' K/V are appended by the
@@ -326,36 +332,8 @@ int run_extend(int op, const void* q, const void* k_pool, const void* v_pool, in
   if (!q || !k_pool || !v_pool || !block_table || !out || !workspace) return TIDE_ERR_INVALID_ARG;
   if (fused && (!k_new || !v_new)) return TIDE_ERR_INVALID_ARG;
   if (workspace_bytes < plan.total_bytes) return TIDE_ERR_CAPACITY;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  Staged st;
-  rc = upload(plan, workspace, s, plan.split ? 0 : (uint32_t)plan.num_items, &st);
-  if (rc != TIDE_OK) return rc;
-  ExtendArgs a;
-  a.reads = st.reads;
-  a.k_new = fused ? static_cast<const uint16_t*>(k_new) : nullptr;
-  a.v_new = fused ? static_cast<const uint16_t*>(v_new) : nullptr;
-  a.q = static_cast<const uint16_t*>(q);
-  a.k_pool = static_cast<const uint16_t*>(k_pool);
-  a.v_pool = static_cast<const uint16_t*>(v_pool);
-  a.block_table = block_table;
-  a.num_pages = num_pages;
-  a.bt_stride = bt_stride;
-  a.num_q_heads = dims->num_q_heads;
-  a.num_kv_heads = dims->num_kv_heads;
-  a.group = dims->num_q_heads / dims->num_kv_heads;
-  a.scale_log2 = dims->sm_scale * 1.44269504088896340736f;
-  a.num_items = plan.num_items;
-  a.tasks = at<TaskDesc>(st.plan, plan.tasks_off);
-  a.items = plan.split ? nullptr : at<ExtendItem>(st.plan, plan.items_off);
-  a.out = static_cast<uint16_t*>(out);
-  a.lse = lse;
-  a.error_flags = at_mut<int32_t>(workspace, 0);
-  a.chunk_items = plan.split ? at<ExtendChunkItem>(workspace, plan.items_off) : nullptr;
-  a.merge_rows = plan.split ? at<MergeRow>(workspace, plan.merge_rows_off) : nullptr;
-  a.part_o = plan.split ? at_mut<float>(workspace, plan.part_o_off) : nullptr;
-  a.part_ml = plan.split ? at_mut<float>(workspace, plan.part_ml_off) : nullptr;
-  a.total_rows = plan.total_rows;
-  return finish(launch_extend(a, dims->head_dim, plan.waves, s), st, workspace, s);
+  return run_extend_plan(plan, q, k_pool, v_pool, num_pages, block_table, bt_stride, *dims, out, lse, workspace,
+                         static_cast<hipStream_t>(stream), fused ? k_new : nullptr, fused ? v_new : nullptr);
 }
 
 // Shared path of tide_decode_attn, tide_decode_append_attn (fused: k_new / v_new) and
@@ -468,6 +446,38 @@ int run_decode(const void* q, const void* k_new, const void* v_new, const void* 
   return finish(launch_decode(a, dims->head_dim, false, s), st, workspace, s);
 }
 
+// The plan of any operation, without its work lists.  An extend over the 4-bit cache that goes by
+// rounds has several: then the first round's, with the whole call's items and workspace.
+int plan_any(int op, int32_t num_tasks, const int32_t* lens_a, const int32_t* lens_b, const tide_dims& dims,
+             int32_t num_splits, Plan* plan) {
+  switch (op) {
+    case TIDE_OP_DECODE:
+      return make_plan_decode(num_tasks, lens_a, dims, num_splits, -1, false, plan);
+    case TIDE_OP_KV4_APPEND:
+    case TIDE_OP_KV4_UNPACK:
+      return make_plan(TIDE_OP_KV_APPEND, num_tasks, lens_a, lens_b, dims, 0, -1, false, plan);
+    case TIDE_OP_KV4_DECODE:
+      return make_plan_kv4_units(op, num_tasks, lens_a, nullptr, dims, -1, false, plan);
+    case TIDE_OP_KV4_EXTEND: {
+      Kv4ExtendPlan x;
+      const int rc = make_plan_kv4_extend(num_tasks, lens_a, lens_b, dims, -1, false, &x);
+      if (rc != TIDE_OK) return rc;
+      *plan = x.by_units ? x.units : x.rounds.empty() ? Plan() : x.rounds[0].extend;
+      int64_t items = x.by_units ? plan->num_items : 0;
+      for (const Kv4Round& r : x.rounds) items += r.extend.num_items;
+      plan->num_items = (int32_t)std::min<int64_t>(items, INT32_MAX);
+      plan->total_bytes = x.total_bytes;
+      return TIDE_OK;
+    }
+    case TIDE_OP_ATTN_MASS:
+      return make_plan_mass(num_tasks, lens_a, lens_b, nullptr, dims, -1, false, plan);
+    case TIDE_OP_KV_EVICT:
+      return make_plan_evict(num_tasks, lens_a, lens_b, nullptr, dims, -1, -1, false, plan);
+    default:
+      return make_plan(op, num_tasks, lens_a, lens_b, dims, num_splits, -1, false, plan);
+  }
+}
+
 }  // namespace
 }  // namespace tide
 
@@ -483,9 +493,7 @@ TIDE_API int tide_workspace_size(int op, int32_t num_tasks, const int32_t* lens_
     int rc = check_dims(dims);
     if (rc != TIDE_OK) return rc;
     Plan plan;
-    rc = op == TIDE_OP_DECODE
-             ? make_plan_decode(num_tasks, lens_a, *dims, num_splits, -1, false, &plan)
-             : make_plan(op, num_tasks, lens_a, lens_b, *dims, num_splits, -1, false, &plan);
+    rc = plan_any(op, num_tasks, lens_a, lens_b, *dims, num_splits, &plan);
     if (rc != TIDE_OK) return rc;
     *bytes_out = plan.total_bytes;
     return TIDE_OK;
@@ -502,22 +510,24 @@ TIDE_API int tide_plan_info_get(int op, int32_t num_tasks, const int32_t* lens_a
     int rc = check_dims(dims);
     if (rc != TIDE_OK) return rc;
     Plan plan;
-    rc = op == TIDE_OP_DECODE
-             ? make_plan_decode(num_tasks, lens_a, *dims, num_splits, -1, false, &plan)
-             : make_plan(op, num_tasks, lens_a, lens_b, *dims, num_splits, -1, false, &plan);
+    rc = plan_any(op, num_tasks, lens_a, lens_b, *dims, num_splits, &plan);
     if (rc != TIDE_OK) return rc;
     *out = tide_plan_info{};
     out->num_items = plan.num_items;
     out->workspace_bytes = plan.total_bytes;
-    if (op == TIDE_OP_DECODE) {
+    if (op == TIDE_OP_KV4_DECODE || op == TIDE_OP_KV4_EXTEND) {
+      out->waves_per_group = plan.stream ? kv4_waves(plan.num_items) : plan.waves;
+      out->run_steps = plan.steps;
+      out->split = plan.split ? 1 : 0;
+    } else if (op == TIDE_OP_DECODE) {
       out->waves_per_group =
           plan.stream ? stream_waves(plan.num_items) : decode_waves(plan.num_items);
       out->max_splits = plan.max_splits;
       out->merge_in_kernel = plan.fold_merge ? 1 : 0;
       out->run_steps = plan.steps;
-    } else if (op == TIDE_OP_KV_APPEND) {
+    } else if (op == TIDE_OP_KV_APPEND || op == TIDE_OP_KV4_APPEND || op == TIDE_OP_KV4_UNPACK) {
       out->waves_per_group = append_waves();
-    } else {
+    } else if (op == TIDE_OP_EXTEND || op == TIDE_OP_FULL_PREFILL) {
       out->waves_per_group = plan.waves;
       out->split = plan.split ? 1 : 0;
     }

@@ -306,4 +306,163 @@ struct StreamArgs {
   PlanReads reads;
 };
 
+// ---- the 4-bit cache ------------------------------------------------------------------------
+// Bytes of one (page, kv head) block: K codes, V codes, K scales, V scales (kv4.h).
+TIDE_HD constexpr int kv4_block_bytes(int head_dim) { return 17 * head_dim; }
+
+// Query rows (tokens x heads of a kv head) of one attention unit: the columns of a 16-wide MFMA.
+constexpr int kKv4Cols = 16;
+
+// Waves per workgroup of such attention, and workgroups, as stream_waves and stream_groups.
+TIDE_HD inline int32_t kv4_waves(int64_t items) { return items > 256 ? 8 : 4; }
+
+TIDE_HD inline int32_t kv4_groups(int32_t runs, int32_t num_kv_heads) {
+  const int32_t waves = kv4_waves((int64_t)runs * num_kv_heads);
+  return (runs + waves - 1) / waves * num_kv_heads;
+}
+
+// Append and unpack: work items are AppendItems.
+struct Kv4StoreArgs {
+  const uint16_t* k_new;  // append
+  const uint16_t* v_new;
+  uint16_t* k_out;        // unpack: rows packed like k_new
+  uint16_t* v_out;
+  uint8_t* pool;
+  const int32_t* block_table;
+  int64_t num_pages;
+  int32_t bt_stride;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t num_items;
+  const TaskDesc* tasks;
+  const AppendItem* items;
+  int32_t* error_flags;
+  PlanReads reads;
+};
+
+// Unpacking whole pages for the extend kernel: pages [lpage, lpage + pages) of block-table row
+// `row` go to pages [to, to + pages) of the bf16 staging pools, and those ids into row `task` of
+// the staging block table.
+struct Kv4StageItem {
+  int32_t row;
+  int32_t lpage;
+  int32_t pages;
+  int32_t to;
+  int32_t task;
+  int32_t pad[3];
+};
+
+struct Kv4StageArgs {
+  const uint8_t* pool;
+  const int32_t* block_table;
+  int64_t num_pages;
+  int32_t bt_stride;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t num_items;
+  const Kv4StageItem* items;
+  uint16_t* k_stage;  // [staging pages][Hkv][kPage][d]
+  uint16_t* v_stage;
+  int32_t* stage_table;  // [tasks][stage_stride]
+  int32_t stage_stride;
+  int32_t* error_flags;
+  PlanReads reads;
+};
+
+// Attention over the 4-bit cache in runs of steps, as StreamArgs.  A task of the plan is a unit:
+// `extend` query tokens (packed rows row_start ..) at positions prefix .. prefix + extend - 1, read
+// through block-table row `aux`; their extend x group rows are the columns of the MFMAs.
+struct Kv4AttnArgs {
+  const uint16_t* q;
+  uint8_t* pool;
+  const int32_t* block_table;
+  int64_t num_pages;
+  int32_t bt_stride;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t group;
+  int32_t cols;  // rows of a partial: the most tokens of a unit x group
+  float scale_log2;
+  int32_t num_runs;
+  int32_t steps;
+  int32_t last_steps;
+  const TaskDesc* units;
+  const StreamItem* items;
+  int32_t num_units;
+  float* part_o;   // [Hkv][slots][cols][d]
+  float* part_ml;  // [Hkv][slots][cols][4]
+  uint64_t* flags;
+  uint64_t call;
+  uint16_t* out;
+  float* lse;
+  int32_t* error_flags;
+  const uint16_t* k_new;  // fused append: one token a unit, [units][Hkv][d]
+  const uint16_t* v_new;
+  PlanReads reads;
+};
+
+// ---- attention mass and eviction ---------------------------------------------------------------
+constexpr int kMassKeys = 256;  // keys of a work item, for every kv head
+
+// Work item: keys [key0, key0 + kMassKeys) of `task`.
+struct MassItem {
+  int32_t task;
+  int32_t key0;
+};
+
+// aux of a task: the positions whose sums are carried on (later ones start at 0).
+struct MassArgs {
+  const uint16_t* q;
+  const float* lse;
+  const void* pool;  // K pages, or the 4-bit pool
+  const int32_t* block_table;
+  int64_t num_pages;
+  int32_t bt_stride;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t group;
+  float scale_log2;
+  int32_t num_items;
+  const TaskDesc* tasks;
+  const MassItem* items;
+  float* mass;
+  int32_t* error_flags;
+  PlanReads reads;
+};
+
+// One task of an eviction: `keep` of `kv_len` positions stay, the last `recent` of them always.
+struct EvictTask {
+  int32_t task;    // block-table row
+  int32_t kv_len;
+  int32_t keep;
+  int32_t recent;
+  int32_t first;   // packed row of `kept`: the sum of the earlier tasks' keep
+  int32_t pad[3];
+};
+
+// A kept position and the page that holds it (-1: out of range, left where it is).
+struct EvictIndex {
+  int32_t pos;
+  int32_t page;
+};
+
+struct EvictArgs {
+  uint8_t* k_pool;  // K pages, or the 4-bit pool
+  uint8_t* v_pool;
+  float* mass;
+  const int32_t* block_table;
+  const int32_t* new_table;  // equal to block_table: in place
+  int64_t num_pages;
+  int32_t bt_stride;
+  int32_t new_stride;
+  int32_t num_kv_heads;
+  int32_t num_tasks;
+  int32_t longest_keep;
+  const EvictTask* tasks;
+  EvictIndex* index;  // [sum of keep x Hkv]: a task's from first x Hkv on, head after head, ascending
+  float* index_mass;  // the kept positions' sums, like index
+  int32_t* kept;      // [sum of keep][Hkv], may be null
+  int32_t* error_flags;
+};
+
 }  // namespace tide
