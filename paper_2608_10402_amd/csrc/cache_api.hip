@@ -141,8 +141,9 @@ int mass(const void* q, const float* lse, const void* pool, bool kv4, int64_t nu
   if (workspace_bytes < plan.total_bytes) return TIDE_ERR_CAPACITY;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Staged st;
-  const int64_t groups = (int64_t)plan.num_items * dims->num_kv_heads;
-  rc = upload(plan, workspace, s, groups <= kInPlaceGroups ? (uint32_t)groups : 0, &st);
+  const uint32_t readers =
+      num_tasks <= plan.num_runs ? mass_groups(plan.num_runs, dims->num_kv_heads, plan.one_trip) : 0;
+  rc = upload(plan, workspace, s, readers, &st);
   if (rc != TIDE_OK) return rc;
   MassArgs a = {};
   a.q = static_cast<const uint16_t*>(q);
@@ -155,9 +156,10 @@ int mass(const void* q, const float* lse, const void* pool, bool kv4, int64_t nu
   a.num_kv_heads = dims->num_kv_heads;
   a.group = dims->num_q_heads / dims->num_kv_heads;
   a.scale_log2 = dims->sm_scale * 1.44269504088896340736f;
-  a.num_items = plan.num_items;
+  a.num_runs = plan.num_runs;
+  a.one_trip = plan.one_trip;
   a.tasks = at<TaskDesc>(st.plan, plan.tasks_off);
-  a.items = at<MassItem>(st.plan, plan.items_off);
+  a.runs = at<MassRun>(st.plan, plan.items_off);
   a.mass = sums;
   a.error_flags = at_mut<int32_t>(workspace, 0);
   a.reads = st.reads;

@@ -474,6 +474,16 @@ hipError_t launch_kv4(const Kv4AttnArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Every variant is instantiated explicitly (see attn_decode.hip).
+template __global__ void kv4_decode_kernel<128, false, kKv4Big>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, false, kKv4Small>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, true, kKv4Big>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, true, kKv4Small>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, false, kKv4Big>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, false, kKv4Small>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, true, kKv4Big>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, true, kKv4Small>(Kv4AttnArgs);
+
 }  // namespace kern
 
 hipError_t launch_kv4_decode(const Kv4AttnArgs& a, int head_dim, hipStream_t stream) {

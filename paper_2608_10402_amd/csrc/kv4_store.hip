@@ -202,6 +202,14 @@ __global__ __launch_bounds__(kStoreWaves * 64) void kv4_stage_kernel(Kv4StageArg
   }
 }
 
+// Every variant is instantiated explicitly (see attn_decode.hip).
+template __global__ void kv4_store_kernel<128, false>(Kv4StoreArgs);
+template __global__ void kv4_store_kernel<128, true>(Kv4StoreArgs);
+template __global__ void kv4_store_kernel<64, false>(Kv4StoreArgs);
+template __global__ void kv4_store_kernel<64, true>(Kv4StoreArgs);
+template __global__ void kv4_stage_kernel<128>(Kv4StageArgs);
+template __global__ void kv4_stage_kernel<64>(Kv4StageArgs);
+
 }  // namespace kern
 
 int kv4_store_groups(int32_t num_kv_heads) {

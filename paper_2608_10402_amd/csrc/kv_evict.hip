@@ -278,6 +278,12 @@ hipError_t launch(const EvictArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Every variant is instantiated explicitly (see attn_decode.hip).
+template __global__ void evict_move_kernel<128, false>(EvictArgs);
+template __global__ void evict_move_kernel<128, true>(EvictArgs);
+template __global__ void evict_move_kernel<64, false>(EvictArgs);
+template __global__ void evict_move_kernel<64, true>(EvictArgs);
+
 }  // namespace kern
 
 hipError_t launch_evict(const EvictArgs& a, int head_dim, bool kv4, hipStream_t stream) {

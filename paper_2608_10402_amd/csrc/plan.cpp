@@ -1000,6 +1000,9 @@ int make_plan_shared(int32_t num_tasks, const int32_t* kv_lens, int32_t num_grou
 namespace {
 
 constexpr int64_t kKv4WaveSlots = 2048;
+constexpr int64_t kMassOneTripSlots = 4096;  // waves the device holds at once: 16 a CU
+constexpr int64_t kMassSlots = 3072;         // 12 a CU
+constexpr int64_t kMassBlockCost = 2;  // reading a block and its sums, in trips of 16 rows
 constexpr int64_t kKv4StageBytes = (int64_t)1 << 30;
 constexpr int32_t kKv4StagePages = 16;  // of a staging item
 constexpr int32_t kKv4DirectTokens = 16;
@@ -1191,8 +1194,11 @@ int make_plan_mass(int32_t num_tasks, const int32_t* prefix_lens, const int32_t*
   plan->op = TIDE_OP_ATTN_MASS;
   plan->num_tasks = num_tasks;
   std::vector<TaskDesc> tasks((size_t)num_tasks);
-  std::vector<MassItem> items;
-  int64_t rows = 0, n_items = 0;
+  const int32_t hkv = dims.num_kv_heads, group = dims.num_q_heads / hkv;
+  int64_t rows = 0, blocks = 0, cost = 0;
+  auto block_cost = [&](const TaskDesc& t) {  // (bounded: costs times runs stay in 64 bits)
+    return kMassBlockCost + std::min<int64_t>(ceil_div((int64_t)t.extend * group, 16), 1 << 20);
+  };
   for (int32_t b = 0; b < num_tasks; ++b) {
     int32_t p = 0, e = 0;
     rc = task_lengths(TIDE_OP_EXTEND, b, prefix_lens, extend_lens, &p, &e);
@@ -1204,22 +1210,45 @@ int make_plan_mass(int32_t num_tasks, const int32_t* prefix_lens, const int32_t*
     if (rows > INT32_MAX) return TIDE_ERR_INVALID_ARG;
     if (bt_stride >= 0 && ceil_div((int64_t)p + e, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
     if (e == 0) continue;
-    n_items += ceil_div((int64_t)p + e, kMassKeys);
-    if (build_blob)
-      for (int64_t k = 0; k < (int64_t)p + e; k += kMassKeys) items.push_back(MassItem{b, (int32_t)k});
+    const int64_t n = ceil_div((int64_t)p + e, kMassKeys);
+    blocks += n;
+    cost += n * block_cost(tasks[b]);
+    plan->tokens_per_item = std::max(plan->tokens_per_item, e);
   }
-  if (n_items * dims.num_kv_heads > INT32_MAX / 4) return TIDE_ERR_INVALID_ARG;
-  plan->num_items = (int32_t)n_items;
+  if (blocks > INT32_MAX) return TIDE_ERR_INVALID_ARG;
+  plan->one_trip = (int64_t)plan->tokens_per_item * group <= 16;
+  const int64_t slots = plan->one_trip ? kMassOneTripSlots : kMassSlots;
+  const int64_t most = std::min(blocks, std::max<int64_t>(1, slots / hkv));
+  // runs of equal cost: run r starts with the block that r / most of the cost lies in
+  std::vector<MassRun> runs;
+  int64_t at = 0;  // cost before the block
+  for (int32_t b = 0; b < num_tasks; ++b) {
+    if (tasks[b].extend == 0) continue;
+    const int64_t each = block_cost(tasks[b]);
+    const int32_t n = (int32_t)ceil_div((int64_t)tasks[b].prefix + tasks[b].extend, kMassKeys);
+    for (int32_t k = 0; k < n;) {
+      if ((int64_t)runs.size() * cost <= at * most) runs.push_back(MassRun{b, k, 0, 0});
+      // blocks until the next run's start
+      const int64_t next = ceil_div(ceil_div((int64_t)runs.size() * cost, most) - at, each);
+      const int32_t take = (int32_t)std::min<int64_t>(n - k, std::max<int64_t>(1, next));
+      runs.back().blocks += take;
+      k += take;
+      at += take * each;
+    }
+  }
+  plan->num_runs = (int32_t)runs.size();
+  if ((int64_t)plan->num_runs * hkv > INT32_MAX / 4) return TIDE_ERR_INVALID_ARG;
+  plan->num_items = plan->num_runs * hkv;
   plan->total_rows = (int32_t)rows;
   size_t off = sizeof(WsHeader);
   plan->tasks_off = off;
   off = align_up(off + tasks.size() * sizeof(TaskDesc), kWsAlign);
   plan->items_off = off;
-  off = align_up(off + (size_t)n_items * sizeof(MassItem), kWsAlign);
+  off = align_up(off + runs.size() * sizeof(MassRun), kWsAlign);
   plan->upload_bytes = plan->total_bytes = off;
   if (!build_blob) return TIDE_OK;
   put(&plan->blob, plan->tasks_off, tasks);
-  put(&plan->blob, plan->items_off, items);
+  put(&plan->blob, plan->items_off, runs);
   plan->blob.resize(plan->upload_bytes, 0);
   return TIDE_OK;
 }

@@ -48,6 +48,7 @@ struct Plan {
   // extend: tokens per work item and waves per workgroup
   int32_t tokens_per_item = 0;
   int32_t waves = 0;
+  bool one_trip = false;  // attention mass: no task has over 16 query rows a kv head
   // extend: passes over the blocks that the search for the chunk length made
   int32_t search_passes = 0;
   int32_t chunk = 0;  // decode: keys per chunk or run; split extend: most key tiles per chunk
@@ -114,7 +115,7 @@ struct Kv4ExtendPlan {
 int make_plan_kv4_extend(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
                          const tide_dims& dims, int32_t bt_stride, bool build_blob, Kv4ExtendPlan* plan);
 
-// Attention mass: MassItems.  counted: positions per task whose sums are carried on (null: prefix).
+// Attention mass: MassRuns.  counted: positions per task whose sums are carried on (null: prefix).
 int make_plan_mass(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
                    const int32_t* counted, const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan);
 
