@@ -250,6 +250,12 @@ def _lens_total(lens):
     return None if (lens < 0).any() else int(lens.sum(dtype=np.int64))
 
 
+def rows_of(lens) -> int:
+    """Packed rows of these per-task counts (0 for counts that the library will refuse)."""
+    arr, _ = _host(lens, "lens")
+    return (_lens_total(arr) or 0) if arr is not None else 0
+
+
 def _pool_shape(k_pool, v_pool, dims):
     shape = k_pool.shape
     if len(shape) != 4 or v_pool.dim() != 4:
@@ -505,21 +511,19 @@ def _pair(a, b, a_name, b_name):
     return a, a_p, b, b_p
 
 
-class _on_device:
-    """Makes the tensors' device the current one for a call (its stream, staging and launches)."""
-
-    def __init__(self, t):
-        self._to = t.get_device() if isinstance(t, torch.Tensor) and t.is_cuda else -1
-
-    def __enter__(self):
-        self._guard = None
-        if self._to >= 0 and self._to != torch.cuda.current_device():
-            self._guard = torch.cuda.device(self._to)
-            self._guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+def _invoke(name, on, stream, *args):
+    """Calls an entry point on the device of `on` (its stream, staging and launches), which need
+    not be the current one."""
+    fn = getattr(load(), name)
+    dev = on.get_device()
+    if dev < 0 or dev == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(dev) if stream is None and _raw_stream is not None and dev >= 0
+                    else _stream(stream))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _stream(stream))
+    if status != TIDE_OK:
+        raise TideError(status, name)
 
 
 def _mass_pool(mass, num_pages, dims):
@@ -537,30 +541,35 @@ def tide_kv4_append(k_new, v_new, kv4_pool, block_table, prefix_lens, extend_len
     _block_table(block_table, int(p.size))
     _same_device(k_new, v_new, kv4_pool, block_table, workspace)
     ws, ws_n = _ws(workspace)
-    with _on_device(kv4_pool):
-        _check(load().tide_kv4_append(
+    _invoke("tide_kv4_append", kv4_pool, stream,
             _dev(k_new, torch.bfloat16, "k_new"), _dev(v_new, torch.bfloat16, "v_new"),
             _dev(kv4_pool, torch.uint8, "kv4_pool"), num_pages,
             _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(p.size),
-            p_p, e_p, ctypes.byref(dims), ws, ws_n, _stream(stream)), "tide_kv4_append")
+            p_p, e_p, ctypes.byref(dims), ws, ws_n)
 
 
-def tide_kv4_unpack(kv4_pool, block_table, prefix_lens, extend_lens, dims: tide_dims, k_out, v_out,
-                    workspace, stream=None) -> None:
+def tide_kv4_unpack(kv4_pool, block_table, prefix_lens, extend_lens, dims: tide_dims, k_out=None,
+                    v_out=None, workspace=None, stream=None):
+    """Returns (k_out, v_out), new ones where they are None."""
     num_pages = _pool4_shape(kv4_pool, dims)
     p, p_p, e, e_p = _pair(prefix_lens, extend_lens, "prefix_lens", "extend_lens")
     rows = _lens_total(e)
+    if k_out is None:
+        k_out = torch.empty((rows or 0, dims.num_kv_heads, dims.head_dim), dtype=torch.bfloat16,
+                            device=kv4_pool.device)
+    if v_out is None:
+        v_out = torch.empty_like(k_out)
     _rows(k_out, "k_out", rows, dims.num_kv_heads, dims.head_dim)
     _rows(v_out, "v_out", rows, dims.num_kv_heads, dims.head_dim)
     _block_table(block_table, int(p.size))
     _same_device(k_out, v_out, kv4_pool, block_table, workspace)
     ws, ws_n = _ws(workspace)
-    with _on_device(kv4_pool):
-        _check(load().tide_kv4_unpack(
+    _invoke("tide_kv4_unpack", kv4_pool, stream,
             _dev(kv4_pool, torch.uint8, "kv4_pool"), num_pages,
             _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(p.size),
             p_p, e_p, ctypes.byref(dims), _dev(k_out, torch.bfloat16, "k_out"),
-            _dev(v_out, torch.bfloat16, "v_out"), ws, ws_n, _stream(stream)), "tide_kv4_unpack")
+            _dev(v_out, torch.bfloat16, "v_out"), ws, ws_n)
+    return k_out, v_out
 
 
 def tide_kv4_decode_attn(q, kv4_pool, block_table, kv_lens, dims: tide_dims, out, lse=None,
@@ -569,13 +578,11 @@ def tide_kv4_decode_attn(q, kv4_pool, block_table, kv_lens, dims: tide_dims, out
     kv, kv_p = _host(kv_lens, "kv_lens")
     _decode_checks(q, out, lse, block_table, kv, dims, kv4_pool, workspace)
     ws, ws_n = _ws(workspace)
-    with _on_device(kv4_pool):
-        _check(load().tide_kv4_decode_attn(
+    _invoke("tide_kv4_decode_attn", kv4_pool, stream,
             _dev(q, torch.bfloat16, "q"), _dev(kv4_pool, torch.uint8, "kv4_pool"), num_pages,
             _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(kv.size),
             kv_p, ctypes.byref(dims), _dev(out, torch.bfloat16, "out"),
-            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n, _stream(stream)),
-            "tide_kv4_decode_attn")
+            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n)
 
 
 def tide_kv4_decode_append_attn(q, k_new, v_new, kv4_pool, block_table, kv_lens, dims: tide_dims,
@@ -586,14 +593,12 @@ def tide_kv4_decode_append_attn(q, k_new, v_new, kv4_pool, block_table, kv_lens,
     _rows(k_new, "k_new", int(kv.size), dims.num_kv_heads, dims.head_dim)
     _rows(v_new, "v_new", int(kv.size), dims.num_kv_heads, dims.head_dim)
     ws, ws_n = _ws(workspace)
-    with _on_device(kv4_pool):
-        _check(load().tide_kv4_decode_append_attn(
+    _invoke("tide_kv4_decode_append_attn", kv4_pool, stream,
             _dev(q, torch.bfloat16, "q"), _dev(k_new, torch.bfloat16, "k_new"),
             _dev(v_new, torch.bfloat16, "v_new"), _dev(kv4_pool, torch.uint8, "kv4_pool"),
             num_pages, _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]),
             int(kv.size), kv_p, ctypes.byref(dims), _dev(out, torch.bfloat16, "out"),
-            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n, _stream(stream)),
-            "tide_kv4_decode_append_attn")
+            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n)
 
 
 def tide_kv4_extend_attn(q, kv4_pool, block_table, prefix_lens, extend_lens, dims: tide_dims, out,
@@ -607,13 +612,11 @@ def tide_kv4_extend_attn(q, kv4_pool, block_table, prefix_lens, extend_lens, dim
     _block_table(block_table, int(p.size))
     _same_device(q, kv4_pool, block_table, out, lse, workspace)
     ws, ws_n = _ws(workspace)
-    with _on_device(kv4_pool):
-        _check(load().tide_kv4_extend_attn(
+    _invoke("tide_kv4_extend_attn", kv4_pool, stream,
             _dev(q, torch.bfloat16, "q"), _dev(kv4_pool, torch.uint8, "kv4_pool"), num_pages,
             _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(p.size),
             p_p, e_p, ctypes.byref(dims), _dev(out, torch.bfloat16, "out"),
-            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n, _stream(stream)),
-            "tide_kv4_extend_attn")
+            _dev(lse, torch.float32, "lse", nullable=True), ws, ws_n)
 
 
 def _attn_mass(name, q, lse, pool, pool_type, num_pages, block_table, prefix_lens, extend_lens,
@@ -627,13 +630,11 @@ def _attn_mass(name, q, lse, pool, pool_type, num_pages, block_table, prefix_len
     _block_table(block_table, int(p.size))
     _same_device(q, lse, pool, block_table, mass, workspace)
     ws, ws_n = _ws(workspace)
-    with _on_device(pool):
-        _check(getattr(load(), name)(
+    _invoke(name, pool, stream,
             _dev(q, torch.bfloat16, "q"), _dev(lse, torch.float32, "lse"),
             _dev(pool, pool_type, "pool"), num_pages,
             _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), int(p.size),
-            p_p, e_p, c_p, ctypes.byref(dims), _dev(mass, torch.float32, "mass"), ws, ws_n,
-            _stream(stream)), name)
+            p_p, e_p, c_p, ctypes.byref(dims), _dev(mass, torch.float32, "mass"), ws, ws_n)
 
 
 def tide_attn_mass(q, lse, k_pool, block_table, prefix_lens, extend_lens, dims: tide_dims, mass,
@@ -673,14 +674,12 @@ def tide_kv_evict(k_pool, v_pool, mass, block_table, kv_lens, keep_lens, dims: t
                                                      kv_lens, keep_lens, recent_lens, kept, dims)
     _same_device(k_pool, v_pool, mass, block_table, new_block_table, kept, workspace)
     ws, ws_n = _ws(workspace)
-    with _on_device(k_pool):
-        _check(load().tide_kv_evict(
+    _invoke("tide_kv_evict", k_pool, stream,
             _dev(k_pool, torch.bfloat16, "k_pool"), _dev(v_pool, torch.bfloat16, "v_pool"),
             _dev(mass, torch.float32, "mass"), num_pages,
             _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), new_p, stride,
             int(hold[0].size), n_p, k_p, r_p, ctypes.byref(dims),
-            _dev(kept, torch.int32, "kept", nullable=True), ws, ws_n, _stream(stream)),
-            "tide_kv_evict")
+            _dev(kept, torch.int32, "kept", nullable=True), ws, ws_n)
 
 
 def tide_kv4_evict(kv4_pool, mass, block_table, kv_lens, keep_lens, dims: tide_dims,
@@ -691,13 +690,11 @@ def tide_kv4_evict(kv4_pool, mass, block_table, kv_lens, keep_lens, dims: tide_d
                                                      kv_lens, keep_lens, recent_lens, kept, dims)
     _same_device(kv4_pool, mass, block_table, new_block_table, kept, workspace)
     ws, ws_n = _ws(workspace)
-    with _on_device(kv4_pool):
-        _check(load().tide_kv4_evict(
+    _invoke("tide_kv4_evict", kv4_pool, stream,
             _dev(kv4_pool, torch.uint8, "kv4_pool"), _dev(mass, torch.float32, "mass"), num_pages,
             _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), new_p, stride,
             int(hold[0].size), n_p, k_p, r_p, ctypes.byref(dims),
-            _dev(kept, torch.int32, "kept", nullable=True), ws, ws_n, _stream(stream)),
-            "tide_kv4_evict")
+            _dev(kept, torch.int32, "kept", nullable=True), ws, ws_n)
 
 
 def tide_shutdown() -> None:

@@ -31,7 +31,7 @@ int store(bool append, const void* k, const void* v, void* pool, int64_t num_pag
   int rc = start(dims, num_tasks, num_pages, bt_stride, &go);
   if (rc != TIDE_OK || !go) return rc;
   Plan plan;
-  rc = make_plan(TIDE_OP_KV_APPEND, num_tasks, prefix_lens, extend_lens, *dims, 0, bt_stride, true, &plan);
+  rc = make_plan_kv4_store(num_tasks, prefix_lens, extend_lens, *dims, bt_stride, true, &plan);
   if (rc != TIDE_OK) return rc;
   if (plan.num_items == 0) return TIDE_OK;
   if (!k || !v || !pool || !block_table || !workspace) return TIDE_ERR_INVALID_ARG;
@@ -58,8 +58,7 @@ int store(bool append, const void* k, const void* v, void* pool, int64_t num_pag
   a.num_kv_heads = dims->num_kv_heads;
   a.head_dim = dims->head_dim;
   a.num_items = plan.num_items;
-  a.tasks = at<TaskDesc>(st.plan, plan.tasks_off);
-  a.items = at<AppendItem>(st.plan, plan.items_off);
+  a.items = at<Kv4StoreItem>(st.plan, plan.items_off);
   a.error_flags = at_mut<int32_t>(workspace, 0);
   return finish(launch_kv4_store(a, s), st, workspace, s);
 }
@@ -91,7 +90,7 @@ int attend_units(const Plan& plan, const void* q, const void* k_new, const void*
   a.steps = plan.steps;
   a.last_steps = plan.last_steps;
   a.units = at<TaskDesc>(st.plan, plan.tasks_off);
-  a.items = at<StreamItem>(st.plan, plan.items_off);
+  a.runs = at<Kv4Run>(st.plan, plan.items_off);
   a.num_units = plan.num_tasks;
   a.part_o = at_mut<float>(workspace, plan.part_o_off);
   a.part_ml = at_mut<float>(workspace, plan.part_ml_off);
@@ -185,7 +184,8 @@ int evict(void* k_pool, void* v_pool, bool kv4, float* sums, int64_t num_pages, 
   if (workspace_bytes < plan.total_bytes) return TIDE_ERR_CAPACITY;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Staged st;
-  rc = upload(plan, workspace, s, 0, &st);  // (two kernels read it)
+  const int64_t readers = (int64_t)plan.num_tasks * dims->num_kv_heads;
+  rc = upload(plan, workspace, s, readers <= kInPlaceGroups ? (uint32_t)readers : 0, &st);
   if (rc != TIDE_OK) return rc;
   EvictArgs a = {};
   a.k_pool = static_cast<uint8_t*>(k_pool);
@@ -199,9 +199,10 @@ int evict(void* k_pool, void* v_pool, bool kv4, float* sums, int64_t num_pages, 
   a.num_kv_heads = dims->num_kv_heads;
   a.num_tasks = plan.num_tasks;
   a.longest_keep = plan.chunk;
-  a.tasks = at<EvictTask>(workspace, plan.tasks_off);
+  a.tasks = at<EvictTask>(st.plan, plan.tasks_off);
+  a.move_tasks = at_mut<EvictTask>(workspace, plan.part_o_off);
+  a.reads = st.reads;
   a.index = at_mut<EvictIndex>(workspace, plan.items_off);
-  a.index_mass = at_mut<float>(workspace, plan.part_ml_off);
   a.kept = kept;
   a.error_flags = at_mut<int32_t>(workspace, 0);
   return finish(launch_evict(a, dims->head_dim, kv4, s), st, workspace, s);

@@ -39,7 +39,12 @@ struct Kv4 {
   static __device__ __forceinline__ int v_scale(int lane) {
     return kVScales + 4 * ((lane >> 4) * kBlocks + (lane & 15) / kVLanes);
   }
-  // bytes of slot `slot`'s entries in a lane of its quad
+  // A row as 16 pieces of kSpan entries: the bytes of piece r of slot `slot` in K's and in V's codes, and
+  // the scale byte of K's (V's: v_scale of the lane 16 (slot / 4) + r, its byte slot % 4)
+  static __device__ __forceinline__ int k_word(int r, int slot) {
+    return ((r >> 2) * 16 + slot) * kLane + (r & 3) * (kLane / 4);
+  }
+  static __device__ __forceinline__ int k_byte(int r, int slot) { return kKScales + 16 * (r / kVLanes) + slot; }
   static __device__ __forceinline__ int v_word(int r, int slot) {
     return kVCodes + ((slot >> 2) * 16 + r) * kLane + (slot & 3) * (kLane / 4);
   }

@@ -23,7 +23,7 @@ namespace kern {
 
 constexpr int kKv4Big = 8, kKv4Small = 4;  // waves per workgroup (kv4_waves)
 
-typedef const __attribute__((address_space(4))) StreamItem const_item;
+typedef const __attribute__((address_space(4))) Kv4Run const_run;
 
 // One step's codes and scales: [page][word], and a page's scale byte of K and 4 of V.
 template <int D>
@@ -103,9 +103,10 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
     c.table = a.block_table + (int64_t)u[3] * a.bt_stride;
     c.steps = (c.prefix + c.tokens + kDecodeStep - 1) / kDecodeStep;
   };
-  const const_item* it = (const const_item*)(a.items + (live ? run : 0));
-  Cursor ld = {it->task, it->step, 0, 0, 0, 0, nullptr};
-  load_unit(ld);
+  const const_run* it = (const const_run*)(a.runs + (live ? run : 0));
+  Cursor ld = {it->unit, it->step, 0, it->desc.prefix, it->desc.extend, it->desc.row_start,
+               a.block_table + (int64_t)it->desc.aux * a.bt_stride};
+  ld.steps = (ld.prefix + ld.tokens + kDecodeStep - 1) / kDecodeStep;
   Cursor cu = ld;
 
   // Loads of the load cursor's step, through zero-length buffers (zeros, no memory access) past

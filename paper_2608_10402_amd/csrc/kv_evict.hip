@@ -5,13 +5,13 @@
 // Select: one workgroup per (task, kv head).  Sums become 32-bit keys that order like them (NaN
 // lowest); three passes over the task's keys count 11, 11 and 10 bits of those that match the
 // digits found so far and so find the smallest key that stays, and how many of its equals; a last
-// pass ranks what stays by prefix sums and writes (position, page) and the sum, in order.
+// pass ranks what stays by prefix sums and writes an EvictIndex for each, in order.
 //
 // Move: K and V rows go from their position to their rank.  Ranks never exceed positions, so in
 // place a workgroup that loads a chunk of rows, waits for all of them (a barrier) and only then
 // stores them is right if it takes its chunks in order: later chunks read positions beyond every
-// slot written so far.  A workgroup does so for one 128-byte column of K's or V's rows; into new
-// pages the chunks are independent and go to workgroups of their own.
+// slot written so far, which also lets it load the next chunk before it stores one.  Into new pages
+// the chunks are independent and go to workgroups of their own.
 #include "kernels.h"
 #include "kv4.h"
 
@@ -20,6 +20,7 @@ namespace kern {
 
 constexpr int kSelect = 1024;  // threads
 constexpr int kBins = 2048;
+constexpr int kHeld = 5;  // chunks of 4 kSelect keys that the threads hold: contexts of up to 20,480 are read once to count
 
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x + 0.0f);  // -0 counts as 0
@@ -57,10 +58,17 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* tmp, uint32
 __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t tmp[2][kSelect / 64];
-  __shared__ uint32_t found[2];  // digit, keys above it
+  __shared__ uint32_t found[3];  // digit, keys above it, keys with it
   const int tid = threadIdx.x;
   const int unit = blockIdx.x / a.num_kv_heads, head = blockIdx.x - unit * a.num_kv_heads;
-  const EvictTask t = a.tasks[unit];
+  __shared__ EvictTask task;
+  if (tid == 0) task = a.tasks[unit];
+  __syncthreads();
+  const EvictTask t = task;
+  if (tid == 0) {
+    if (a.reads.done) plan_read(a.reads, blockIdx.x);
+    if (head == 0) a.move_tasks[unit] = t;  // for the move, which comes after the slot's release
+  }
   const int32_t* row = a.block_table + (int64_t)t.task * a.bt_stride;
   const int n = t.kv_len, cand = n - t.recent, want = t.keep - t.recent;
 
@@ -79,6 +87,14 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
   // the `want` largest keys of the candidates: those above `least`, and the first `equal` equals
   uint32_t least = 0, equal = 0;
   if (want > 0 && want < cand) {
+    uint32_t held[kHeld][4];
+#pragma unroll
+    for (int c = 0; c < kHeld; ++c) {
+      const int p = 4 * (tid + c * kSelect);
+      float m[4];
+      int32_t page;
+      if (p < cand) load4(p, held[c], m, &page);
+    }
     uint32_t prefix = 0, mask = 0, rest = want;
     constexpr int kShift[3] = {21, 10, 0}, kWidth[3] = {11, 11, 10};
 #pragma unroll
@@ -86,26 +102,39 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
       for (int i = tid; i < kBins; i += kSelect) hist[i] = 0;
       __syncthreads();
       const uint32_t digits = (1u << kWidth[pass]) - 1;
-      for (int p = 4 * tid; p < cand; p += 4 * kSelect) {
+      auto count = [&](const uint32_t (&key)[4], int p) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (p + i < cand && (key[i] & mask) == prefix) atomicAdd(&hist[(key[i] >> kShift[pass]) & digits], 1u);
+      };
+#pragma unroll
+      for (int c = 0; c < kHeld; ++c) count(held[c], 4 * (tid + c * kSelect));
+      for (int p = 4 * (tid + kHeld * kSelect); p < cand; p += 4 * kSelect) {
         uint32_t key[4];
         float m[4];
         int32_t page;
         load4(p, key, m, &page);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (p + i < cand && (key[i] & mask) == prefix) atomicAdd(&hist[(key[i] >> kShift[pass]) & digits], 1u);
+        count(key, p);
       }
       __syncthreads();
       // bins from the largest digit down, two a thread
       const uint32_t hi = hist[kBins - 1 - 2 * tid], lo = hist[kBins - 2 - 2 * tid];
       uint32_t all;
       const uint32_t before = block_scan(hi + lo, tmp[0], &all);
-      if (before < rest && before + hi >= rest) found[0] = kBins - 1 - 2 * tid, found[1] = before;
-      else if (before + hi < rest && before + hi + lo >= rest) found[0] = kBins - 2 - 2 * tid, found[1] = before + hi;
+      if (before < rest && before + hi >= rest)
+        found[0] = kBins - 1 - 2 * tid, found[1] = before, found[2] = hi;
+      else if (before + hi < rest && before + hi + lo >= rest)
+        found[0] = kBins - 2 - 2 * tid, found[1] = before + hi, found[2] = lo;
       __syncthreads();
       prefix |= found[0] << kShift[pass];
       mask |= digits << kShift[pass];
       rest -= found[1];
+      if (rest == found[2]) {  // every key that begins with these digits stays
+        rest = 0;
+        --prefix;  // (not 0: some candidate does not stay)
+        break;
+      }
+      __syncthreads();  // (before found is written again)
     }
     least = prefix;
     equal = rest;
@@ -113,6 +142,7 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
   const bool all_stay = want == cand;
 
   const int64_t out0 = (int64_t)t.first * a.num_kv_heads + (int64_t)head * t.keep;
+  const int32_t* to_row = a.new_table + (int64_t)t.task * a.new_stride;
   uint32_t above = 0, equals = 0;  // positions before the chunk
   int flip = 0;
   for (int p0 = 0; p0 < n; p0 += 4 * kSelect, flip ^= 1) {
@@ -136,8 +166,10 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
       const bool is_eq = eq >> i & 1;
       if ((gt >> i & 1) || (is_eq && e < equal)) {
         const int rank = (int)(g + min(e, equal));
-        a.index[out0 + rank] = EvictIndex{p + i, page};
-        a.index_mass[out0 + rank] = m[i];
+        const int32_t to = to_row[rank / kPage];
+        const bool ok = to >= 0 && to < a.num_pages;
+        if (!ok) atomicOr(a.error_flags, 1);
+        a.index[out0 + rank] = EvictIndex{p + i, ok ? page : -1, to, m[i]};
         if (a.kept) a.kept[((int64_t)t.first + rank) * a.num_kv_heads + head] = p + i;
       }
       g += gt >> i & 1;
@@ -148,15 +180,19 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
   }
 }
 
-constexpr int kMove = 256;  // threads
-constexpr int kInFlight = 8;
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
-// The pieces of one token's row that a part of the move takes: kLanes lanes of kBytes each.
-//   bf16   128-byte columns of K, then of V
-//   4 bit  K codes with their scales, V codes with theirs
+constexpr int kMove = 1024;  // threads
+// Rows a thread has under way, in each of two chunks.  The move is bound by memory where the rows of a
+// workgroup's two chunks cover its latency: 64 tasks cut to half of 2k-16k positions in place (28 / 4
+// heads, d = 128, bf16), call us: 512 threads with 4 rows 298, 6 282, 8 274, 1024 with 4 246, which is
+// the rate of a large copy (4.8 TB/s); with the positions looked up behind the last chunk's rows 349.
+constexpr int kInFlight = 4;
+
+// The pieces of one token's K or V row: kLanes lanes of kBytes each.
 template <int D, bool kKv4, bool kV>
 struct MoveRow {
-  static constexpr int kLanes = kKv4 ? (kV ? 16 : 4) : 8;
+  static constexpr int kLanes = kKv4 ? (kV ? 16 : 4) : D / 8;
   static constexpr int kBytes = kKv4 ? (kV ? D / 32 : D / 8) : 16;
 };
 
@@ -186,20 +222,19 @@ struct Piece {
 };
 
 template <int D, bool kKv4, bool kV>
-__device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictTask& t, int head, int column,
-                                          int chunk_first, int chunk_step) {
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictTask& t, int head, int chunk_first,
+                                          int chunk_step) {
   using M = MoveRow<D, kKv4, kV>;
   using F = Kv4<D>;
   constexpr int kRows = kMove / M::kLanes;  // rows a load
   constexpr int kChunk = kRows * kInFlight;
   const int lane = threadIdx.x % M::kLanes, r0 = threadIdx.x / M::kLanes;
   const int64_t out0 = (int64_t)t.first * a.num_kv_heads + (int64_t)head * t.keep;
-  const int32_t* to_row = a.new_table + (int64_t)t.task * a.new_stride;
   uint8_t* pool = kV && !kKv4 ? a.v_pool : a.k_pool;
   constexpr int64_t kBlk = kKv4 ? F::kBlock : (int64_t)kPage * D * 2;
   auto piece_at = [&](int32_t page, int slot) {
     uint8_t* blk = pool + ((int64_t)page * a.num_kv_heads + head) * kBlk;
-    if constexpr (!kKv4) return blk + slot * D * 2 + 128 * column + 16 * lane;
+    if constexpr (!kKv4) return blk + slot * D * 2 + 16 * lane;
     else if constexpr (kV) return blk + F::v_word(lane, slot);
     else return blk + (16 * lane + slot) * F::kLane;
   };
@@ -210,59 +245,88 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictTask& t
     if constexpr (kV) return blk + F::v_scale(16 * (slot >> 2) + lane) + (slot & 3);
     else return blk + F::k_scale(16 * lane + slot);
   };
-  for (int c0 = chunk_first * kChunk; c0 < t.keep; c0 += chunk_step * kChunk) {
+  struct Chunk {
     Piece<M::kBytes> x[kInFlight];
-    uint8_t scale[kInFlight];
+    uint32_t scale[kInFlight];
     int32_t to[kInFlight];  // page, or -1: not moved
+  };
+  i32x4 rec[kInFlight];  // EvictIndex of the next chunk's rows
+  auto fetch = [&](int c0) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i) {
       const int r = c0 + i * kRows + r0;
-      to[i] = -1;
-      if (r < t.keep) {
-        const EvictIndex from = a.index[out0 + r];
-        const int32_t g = to_row[r / kPage];
-        const bool ok = g >= 0 && g < a.num_pages;
-        if (!ok && lane == 0) atomicOr(a.error_flags, 1);
-        if (ok && from.page >= 0 && (from.page != g || from.pos % kPage != r % kPage)) {
-          to[i] = g;
-          x[i].load(piece_at(from.page, from.pos % kPage));
-          if (scale_lane) scale[i] = *scale_at(from.page, from.pos % kPage);
-        }
+      rec[i] = *reinterpret_cast<const i32x4*>(a.index + out0 + min(r, t.keep - 1));
+    }
+  };
+  auto load = [&](Chunk& c, int c0) {
+#pragma unroll
+    for (int i = 0; i < kInFlight; ++i) {
+      const int r = c0 + i * kRows + r0, pos = rec[i][0], from = rec[i][1], to = rec[i][2];
+      c.to[i] = -1;
+      if (r < t.keep && from >= 0 && (from != to || pos % kPage != r % kPage)) {
+        c.to[i] = to;
+        c.x[i].load(piece_at(from, pos % kPage));
+        if (scale_lane) c.scale[i] = *scale_at(from, pos % kPage);
       }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's rows are here; after the barrier, all of the chunk's
-    __syncthreads();
+    fetch(c0 + chunk_step * kChunk);
+  };
+  auto store = [&](const Chunk& c, int c0) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i) {
       const int slot = (c0 + i * kRows + r0) % kPage;
-      if (to[i] < 0) continue;
-      x[i].store(piece_at(to[i], slot));
-      if (scale_lane) *scale_at(to[i], slot) = scale[i];
+      if (c.to[i] < 0) continue;
+      c.x[i].store(piece_at(c.to[i], slot));
+      if (scale_lane) *scale_at(c.to[i], slot) = (uint8_t)c.scale[i];
     }
+  };
+  // this thread's rows of the chunk are in registers
+  auto arrive = [](Chunk& c) {
+#pragma unroll
+    for (int i = 0; i < kInFlight; ++i) {
+      asm volatile("" : "+v"(c.scale[i])::"memory");
+#pragma unroll
+      for (int w = 0; w < (int)(sizeof(c.x[0].w) / 4); ++w) asm volatile("" : "+v"(c.x[i].w[w])::"memory");
+    }
+  };
+  const int step = chunk_step * kChunk;
+  if (chunk_first * kChunk >= t.keep) return;
+  Chunk even, odd;
+  fetch(chunk_first * kChunk);
+  load(even, chunk_first * kChunk);
+  for (int c0 = chunk_first * kChunk; c0 < t.keep; c0 += 2 * step) {
+    load(odd, c0 + step);
+    arrive(even);
+    __syncthreads();
+    store(even, c0);
+    if (c0 + step >= t.keep) break;
+    load(even, c0 + 2 * step);
+    arrive(odd);
+    __syncthreads();
+    store(odd, c0 + step);
   }
 }
 
 // The kept positions' sums, to the slots of their ranks (read from the index: no order needed).
 __device__ __forceinline__ void move_mass(const EvictArgs& a, const EvictTask& t, int head, int first, int step) {
   const int64_t out0 = (int64_t)t.first * a.num_kv_heads + (int64_t)head * t.keep;
-  const int32_t* to_row = a.new_table + (int64_t)t.task * a.new_stride;
   for (int r = first; r < t.keep; r += step) {
-    const int32_t g = to_row[r / kPage];
-    if (g >= 0 && g < a.num_pages && a.index[out0 + r].page >= 0)
-      a.mass[((int64_t)g * a.num_kv_heads + head) * kPage + r % kPage] = a.index_mass[out0 + r];
+    const EvictIndex x = a.index[out0 + r];
+    if (x.from >= 0) a.mass[((int64_t)x.to * a.num_kv_heads + head) * kPage + r % kPage] = x.mass;
   }
 }
 
-// grid: (task, kv head) x parts (K columns, V columns, sums) x chunk groups
+// grid: (task, kv head) x (K, V with the sums) x chunk groups
 template <int D, bool kKv4>
 __global__ __launch_bounds__(kMove) void evict_move_kernel(EvictArgs a) {
-  constexpr int kCols = kKv4 ? 1 : D / 64;
   const int unit = blockIdx.x / a.num_kv_heads, head = blockIdx.x - unit * a.num_kv_heads;
-  const EvictTask t = a.tasks[unit];
-  const int part = blockIdx.y;
-  if (part < kCols) move_rows<D, kKv4, false>(a, t, head, part, blockIdx.z, gridDim.z);
-  else if (part < 2 * kCols) move_rows<D, kKv4, true>(a, t, head, part - kCols, blockIdx.z, gridDim.z);
-  else move_mass(a, t, head, blockIdx.z * kMove + threadIdx.x, gridDim.z * kMove);
+  const EvictTask t = a.move_tasks[unit];
+  if (blockIdx.y == 0) {
+    move_rows<D, kKv4, false>(a, t, head, blockIdx.z, gridDim.z);
+  } else {
+    move_rows<D, kKv4, true>(a, t, head, blockIdx.z, gridDim.z);
+    move_mass(a, t, head, blockIdx.z * kMove + threadIdx.x, gridDim.z * kMove);
+  }
 }
 
 template <int D, bool kKv4>
@@ -271,10 +335,9 @@ hipError_t launch(const EvictArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(evict_select_kernel, dim3(units), dim3(kSelect), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int kParts = 2 * (kKv4 ? 1 : D / 64) + 1;
-  // in place one workgroup takes a column's chunks in order
+  // in place one workgroup takes its rows' chunks in order
   const unsigned chunks = a.new_table == a.block_table ? 1u : (unsigned)min(64, (a.longest_keep + 255) / 256);
-  hipLaunchKernelGGL((evict_move_kernel<D, kKv4>), dim3(units, kParts, chunks), dim3(kMove), 0, stream, a);
+  hipLaunchKernelGGL((evict_move_kernel<D, kKv4>), dim3(units, 2, chunks), dim3(kMove), 0, stream, a);
   return hipGetLastError();
 }
 

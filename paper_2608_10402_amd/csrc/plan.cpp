@@ -1004,7 +1004,8 @@ constexpr int64_t kMassOneTripSlots = 4096;  // waves the device holds at once: 
 constexpr int64_t kMassSlots = 3072;         // 12 a CU
 constexpr int64_t kMassBlockCost = 2;  // reading a block and its sums, in trips of 16 rows
 constexpr int64_t kKv4StageBytes = (int64_t)1 << 30;
-constexpr int32_t kKv4StagePages = 16;  // of a staging item
+constexpr int32_t kKv4StagePages = 16;  // most pages of a staging item
+constexpr int64_t kKv4StageItems = 1024;  // items that a short call is cut into
 constexpr int32_t kKv4DirectTokens = 16;
 
 // Appends `n` records to a plan's blob region at `off` (grown to its end) and returns the end.
@@ -1017,6 +1018,43 @@ size_t put(std::vector<uint8_t>* blob, size_t off, const std::vector<T>& v) {
 }
 
 }  // namespace
+
+int make_plan_kv4_store(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
+                        const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan) {
+  if (!plan || num_tasks < 0 || (num_tasks > 0 && (!prefix_lens || !extend_lens))) return TIDE_ERR_INVALID_ARG;
+  int rc = check_dims(&dims);
+  if (rc != TIDE_OK) return rc;
+  *plan = Plan();
+  plan->op = TIDE_OP_KV4_APPEND;
+  plan->num_tasks = num_tasks;
+  std::vector<Kv4StoreItem> items;
+  int64_t rows = 0, n_items = 0;
+  for (int32_t b = 0; b < num_tasks; ++b) {
+    int32_t p = 0, e = 0;
+    rc = task_lengths(TIDE_OP_EXTEND, b, prefix_lens, extend_lens, &p, &e);
+    if (rc != TIDE_OK) return rc;
+    if (rows + e > INT32_MAX) return TIDE_ERR_INVALID_ARG;
+    const int64_t end = (int64_t)p + e;
+    if (bt_stride >= 0 && ceil_div(end, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
+    if (e > 0) n_items += (end - 1) / kPage - p / kPage + 1;
+    for (int64_t pos = p; build_blob && pos < end;) {
+      const int64_t to = std::min(end, (pos / kPage + 1) * kPage);
+      items.push_back(Kv4StoreItem{b, (int32_t)(pos / kPage), (int32_t)(rows + pos - p),
+                                   (int32_t)(pos % kPage + 32 * (to - pos))});
+      pos = to;
+    }
+    rows += e;
+  }
+  if (n_items > INT32_MAX / 4) return TIDE_ERR_INVALID_ARG;
+  plan->num_items = (int32_t)n_items;
+  plan->total_rows = (int32_t)rows;
+  plan->items_off = sizeof(WsHeader);
+  plan->upload_bytes = plan->total_bytes = align_up(plan->items_off + (size_t)n_items * sizeof(Kv4StoreItem), kWsAlign);
+  if (!build_blob) return TIDE_OK;
+  put(&plan->blob, plan->items_off, items);
+  plan->blob.resize(plan->upload_bytes, 0);
+  return TIDE_OK;
+}
 
 int make_plan_kv4_units(int op, int32_t num_tasks, const int32_t* lens_a, const int32_t* lens_b,
                         const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan) {
@@ -1070,7 +1108,7 @@ int make_plan_kv4_units(int op, int32_t num_tasks, const int32_t* lens_a, const 
   plan->tasks_off = off;
   off = align_up(off + units.size() * sizeof(TaskDesc), kWsAlign);
   plan->items_off = off;
-  off = align_up(off + (size_t)plan->num_runs * sizeof(StreamItem), kWsAlign);
+  off = align_up(off + (size_t)plan->num_runs * sizeof(Kv4Run), kWsAlign);
   const StreamSlots per_head = {plan->num_runs, plan->num_tasks, kv4_waves(plan->num_items)};
   plan->tickets_off = off;  // the parts' flags
   off = align_up(off + (size_t)per_head.count() * hkv * sizeof(uint64_t), kWsAlign);
@@ -1084,13 +1122,13 @@ int make_plan_kv4_units(int op, int32_t num_tasks, const int32_t* lens_a, const 
   if (!build_blob) return TIDE_OK;
   plan->blob.assign(plan->upload_bytes, 0);
   memcpy(plan->blob.data() + plan->tasks_off, units.data(), units.size() * sizeof(TaskDesc));
-  StreamItem* items = reinterpret_cast<StreamItem*>(plan->blob.data() + plan->items_off);
+  Kv4Run* runs = reinterpret_cast<Kv4Run*>(plan->blob.data() + plan->items_off);
   int64_t at = 0, run = 0;  // first step of the unit, next run to place
   for (size_t u = 0; u < units.size(); ++u) {
     const int32_t kv_len = units[u].prefix + units[u].extend;
     const int64_t end = at + ceil_div(kv_len, kDecodeStep);
     for (; run * steps < end; ++run)
-      items[run] = StreamItem{(int32_t)u, (int32_t)(run * steps - at), kv_len, 0};
+      runs[run] = Kv4Run{(int32_t)u, (int32_t)(run * steps - at), units[u], {0, 0}};
     at = end;
   }
   return TIDE_OK;
@@ -1149,10 +1187,11 @@ int make_plan_kv4_extend(int32_t num_tasks, const int32_t* prefix_lens, const in
     if (rc != TIDE_OK) return rc;
     std::vector<Kv4StageItem> items;
     int64_t to = 0;
+    const int64_t per = std::max<int64_t>(1, std::min<int64_t>(kKv4StagePages, r.pages / kKv4StageItems));
     for (int32_t i = 0; i < r.tasks; ++i) {
       const int64_t n = pages_of(r.first + i);
-      for (int64_t lp = 0; lp < n; lp += kKv4StagePages) {
-        const int32_t k = (int32_t)std::min<int64_t>(kKv4StagePages, n - lp);
+      for (int64_t lp = 0; lp < n; lp += per) {
+        const int32_t k = (int32_t)std::min<int64_t>(per, n - lp);
         items.push_back(Kv4StageItem{r.first + i, (int32_t)lp, k, (int32_t)to, i, {0, 0, 0}});
         to += k;
       }
@@ -1282,11 +1321,11 @@ int make_plan_evict(int32_t num_tasks, const int32_t* kv_lens, const int32_t* ke
   plan->tasks_off = off;
   off = align_up(off + tasks.size() * sizeof(EvictTask), kWsAlign);
   plan->upload_bytes = off;
+  plan->part_o_off = off;  // the tasks again, for the second kernel
+  off = align_up(off + tasks.size() * sizeof(EvictTask), kWsAlign);
   const size_t n = (size_t)kept * dims.num_kv_heads;
   plan->items_off = off;
   off = align_up(off + n * sizeof(EvictIndex), kWsAlign);
-  plan->part_ml_off = off;
-  off = align_up(off + n * sizeof(float), kWsAlign);
   plan->total_bytes = off;
   if (!build_blob) return TIDE_OK;
   put(&plan->blob, plan->tasks_off, tasks);

@@ -87,6 +87,10 @@ int make_plan_shared(int32_t num_tasks, const int32_t* kv_lens, int32_t num_grou
                      bool build_blob, Plan* plan);
 
 // ---- the 4-bit cache, attention mass, eviction ----------------------------------------------
+// Append and unpack: Kv4StoreItems.
+int make_plan_kv4_store(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
+                        const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan);
+
 // Runs of steps over units of up to kKv4Cols / G query tokens each (Kv4AttnArgs).  lens_a, lens_b as
 // TIDE_OP_KV4_DECODE or TIDE_OP_KV4_EXTEND take them.
 int make_plan_kv4_units(int op, int32_t num_tasks, const int32_t* lens_a, const int32_t* lens_b,
@@ -119,7 +123,7 @@ int make_plan_kv4_extend(int32_t num_tasks, const int32_t* prefix_lens, const in
 int make_plan_mass(int32_t num_tasks, const int32_t* prefix_lens, const int32_t* extend_lens,
                    const int32_t* counted, const tide_dims& dims, int32_t bt_stride, bool build_blob, Plan* plan);
 
-// Eviction: EvictTasks (at tasks_off); the index at items_off, its sums at part_ml_off.  recent may be
+// Eviction: EvictTasks (at tasks_off, room for a copy at part_o_off); the index at items_off.  recent may be
 // null (0 everywhere); new_stride < 0: the new pages' capacity is not checked.
 int make_plan_evict(int32_t num_tasks, const int32_t* kv_lens, const int32_t* keep_lens, const int32_t* recent,
                     const tide_dims& dims, int32_t bt_stride, int32_t new_stride, bool build_blob, Plan* plan);

@@ -455,7 +455,7 @@ int plan_any(int op, int32_t num_tasks, const int32_t* lens_a, const int32_t* le
       return make_plan_decode(num_tasks, lens_a, dims, num_splits, -1, false, plan);
     case TIDE_OP_KV4_APPEND:
     case TIDE_OP_KV4_UNPACK:
-      return make_plan(TIDE_OP_KV_APPEND, num_tasks, lens_a, lens_b, dims, 0, -1, false, plan);
+      return make_plan_kv4_store(num_tasks, lens_a, lens_b, dims, -1, false, plan);
     case TIDE_OP_KV4_DECODE:
       return make_plan_kv4_units(op, num_tasks, lens_a, nullptr, dims, -1, false, plan);
     case TIDE_OP_KV4_EXTEND: {

@@ -321,7 +321,16 @@ TIDE_HD inline int32_t kv4_groups(int32_t runs, int32_t num_kv_heads) {
   return (runs + waves - 1) / waves * num_kv_heads;
 }
 
-// Append and unpack: work items are AppendItems.
+// Append and unpack item: slots [s0, s0 + n) of logical page `lpage` of block-table row `task`, packed
+// rows row0 .. row0 + n - 1.  One record has it all: read where it was staged, a second one that
+// depends on it cost another 1.5 us.
+struct Kv4StoreItem {
+  int32_t task;
+  int32_t lpage;
+  int32_t row0;
+  int32_t span;  // s0 + 32 n: scalar loads have no 16-bit form
+};
+
 struct Kv4StoreArgs {
   const uint16_t* k_new;  // append
   const uint16_t* v_new;
@@ -334,8 +343,7 @@ struct Kv4StoreArgs {
   int32_t num_kv_heads;
   int32_t head_dim;
   int32_t num_items;
-  const TaskDesc* tasks;
-  const AppendItem* items;
+  const Kv4StoreItem* items;
   int32_t* error_flags;
   PlanReads reads;
 };
@@ -369,6 +377,15 @@ struct Kv4StageArgs {
   PlanReads reads;
 };
 
+// A run of steps: it starts with step `step` of unit `unit`, whose description it repeats (as
+// Kv4StoreItem does) and may cross into the next units.
+struct Kv4Run {
+  int32_t unit;
+  int32_t step;
+  TaskDesc desc;
+  int32_t pad[2];
+};
+
 // Attention over the 4-bit cache in runs of steps, as StreamArgs.  A task of the plan is a unit:
 // `extend` query tokens (packed rows row_start ..) at positions prefix .. prefix + extend - 1, read
 // through block-table row `aux`; their extend x group rows are the columns of the MFMAs.
@@ -387,7 +404,7 @@ struct Kv4AttnArgs {
   int32_t steps;
   int32_t last_steps;
   const TaskDesc* units;
-  const StreamItem* items;
+  const Kv4Run* runs;
   int32_t num_units;
   float* part_o;   // [Hkv][slots][cols][d]
   float* part_ml;  // [Hkv][slots][cols][4]
@@ -452,10 +469,13 @@ struct EvictTask {
   int32_t pad[3];
 };
 
-// A kept position and the page that holds it (-1: out of range, left where it is).
+// A kept position: its sum, and the pages that it leaves and that its rank lies in (leaves < 0: one of
+// them is out of range, the position is not moved).
 struct EvictIndex {
   int32_t pos;
-  int32_t page;
+  int32_t from;
+  int32_t to;
+  float mass;
 };
 
 struct EvictArgs {
@@ -471,10 +491,11 @@ struct EvictArgs {
   int32_t num_tasks;
   int32_t longest_keep;
   const EvictTask* tasks;
+  EvictTask* move_tasks;  // the same in the workspace, written by the first kernel for the second
   EvictIndex* index;  // [sum of keep x Hkv]: a task's from first x Hkv on, head after head, ascending
-  float* index_mass;  // the kept positions' sums, like index
   int32_t* kept;      // [sum of keep][Hkv], may be null
   int32_t* error_flags;
+  PlanReads reads;
 };
 
 }  // namespace tide

@@ -66,8 +66,7 @@ class _Paged:
 
     def _evict(self, entry, mass, kv_lens, keep_lens, recent_lens, new_block_table, kept, stream):
         if kept is None:
-            rows = int(np.asarray(keep_lens, dtype=np.int64).sum())
-            kept = torch.empty((max(rows, 0), self.dims.num_kv_heads), dtype=torch.int32,
+            kept = torch.empty((_lib.rows_of(keep_lens), self.dims.num_kv_heads), dtype=torch.int32,
                                device=self.device)
         self._call(lambda: _lib.tide_workspace_size(_lib.TIDE_OP_KV_EVICT, kv_lens, keep_lens,
                                                     self.dims),
@@ -222,16 +221,12 @@ class PagedKV4(_Paged):
 
     def unpack(self, prefix_lens, extend_lens, k_out=None, v_out=None, stream=None):
         """The values at positions prefix .. prefix + extend - 1 as bf16 rows (K, V)."""
-        shape = (max(0, int(np.asarray(extend_lens, dtype=np.int64).sum())), self.dims.num_kv_heads,
-                 self.dims.head_dim)
-        if k_out is None:
-            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        if v_out is None:
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        got = []
         self._call(self._size(_lib.TIDE_OP_KV4_UNPACK, prefix_lens, extend_lens),
-                   lambda ws: _lib.tide_kv4_unpack(self.pool, self.block_table, prefix_lens,
-                                                   extend_lens, self.dims, k_out, v_out, ws, stream))
-        return k_out, v_out
+                   lambda ws: got.extend(_lib.tide_kv4_unpack(
+                       self.pool, self.block_table, prefix_lens, extend_lens, self.dims, k_out,
+                       v_out, ws, stream)))
+        return tuple(got)
 
     def decode(self, q, kv_lens, out=None, lse=None, stream=None):
         out = torch.empty_like(q) if out is None else out

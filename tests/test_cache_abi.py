@@ -122,7 +122,7 @@ def size(op, a, b=None, dims=GOOD):
 
 
 def test_workspace_sizes():
-    assert size(tide.TIDE_OP_KV4_APPEND, [3], [5]) == size(tide.TIDE_OP_KV_APPEND, [3], [5])
+    assert 0 < size(tide.TIDE_OP_KV4_APPEND, [3], [5]) <= size(tide.TIDE_OP_KV_APPEND, [3], [5])
     assert size(tide.TIDE_OP_KV4_EXTEND, [5000], [4]) < 1 << 22                 # the codes themselves
     staged = size(tide.TIDE_OP_KV4_EXTEND, [5000], [500])
     assert staged > 5500 * 4 * 128 * 4                                         # K and V of the task in bf16
