@@ -92,6 +92,7 @@ int attend_units(const Plan& plan, const void* q, const void* k_new, const void*
   a.units = at<TaskDesc>(st.plan, plan.tasks_off);
   a.runs = at<Kv4Run>(st.plan, plan.items_off);
   a.num_units = plan.num_tasks;
+  a.reread = plan.reread;
   a.part_o = at_mut<float>(workspace, plan.part_o_off);
   a.part_ml = at_mut<float>(workspace, plan.part_ml_off);
   a.flags = at_mut<uint64_t>(workspace, plan.tickets_off);

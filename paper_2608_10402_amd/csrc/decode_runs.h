@@ -136,7 +136,7 @@ struct RunParts {
   }
 
   // Combines the `len` consecutive waves' partials of one task that lie in LDS from lds_o (outputs,
-  // row j at 4 D j, its 16-byte granule g at g ^ j) and lds_s (statistics, 16 bytes a row), a
+  // row j at 4 D j, its 16-byte granule g at g ^ (j % 16)) and lds_s (statistics, 16 bytes a row), a
   // wave's `stride` and `stride_s` bytes behind the last one's; whole: the unit lies inside this workgroup.
   template <int L>
   __device__ __forceinline__ void combine(const uint8_t* lds_o, const uint8_t* lds_s, int stride, int stride_s, int len,
@@ -155,7 +155,7 @@ struct RunParts {
         f32x4 po[RM::kV];
 #pragma unroll
         for (int k = 0; k < RM::kV; ++k)
-          po[k] = *reinterpret_cast<const f32x4*>(xo + 16 * ((RM::kV * sub + k) ^ jr));
+          po[k] = *reinterpret_cast<const f32x4*>(xo + 16 * ((RM::kV * sub + k) ^ (jr & 15)));
         rm.raise(ml[0]);
         rm.add(ml, po);
       }

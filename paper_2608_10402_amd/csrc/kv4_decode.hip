@@ -31,23 +31,23 @@ struct Kv4Regs {
   uint32_t k[2][Kv4<D>::kWords], v[2][Kv4<D>::kWords], ks[2], vs[2];
 };
 
-template <int D>
+template <int D, int kPolicy>
 __device__ __forceinline__ void kv4_load_page(Kv4Regs<D>& r, int t, __amdgpu_buffer_rsrc_t blk, int lane) {
   using F = Kv4<D>;
   if constexpr (D == 128) {
-    const u32x4 k = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(blk, lane * 16, 0, kStreamPolicy));
+    const u32x4 k = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(blk, lane * 16, 0, kPolicy));
     const u32x4 v = __builtin_bit_cast(
-        u32x4, __builtin_amdgcn_raw_buffer_load_b128(blk, F::kVCodes + lane * 16, 0, kStreamPolicy));
+        u32x4, __builtin_amdgcn_raw_buffer_load_b128(blk, F::kVCodes + lane * 16, 0, kPolicy));
 #pragma unroll
     for (int w = 0; w < 4; ++w) r.k[t][w] = k[w], r.v[t][w] = v[w];
   } else {
-    const uint2 k = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(blk, lane * 8, 0, kStreamPolicy));
+    const uint2 k = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(blk, lane * 8, 0, kPolicy));
     const uint2 v = __builtin_bit_cast(
-        uint2, __builtin_amdgcn_raw_buffer_load_b64(blk, F::kVCodes + lane * 8, 0, kStreamPolicy));
+        uint2, __builtin_amdgcn_raw_buffer_load_b64(blk, F::kVCodes + lane * 8, 0, kPolicy));
     r.k[t][0] = k.x, r.k[t][1] = k.y, r.v[t][0] = v.x, r.v[t][1] = v.y;
   }
-  r.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(blk, F::k_scale(lane), 0, kStreamPolicy);
-  r.vs[t] = __builtin_amdgcn_raw_buffer_load_b32(blk, F::v_scale(lane), 0, kStreamPolicy);
+  r.ks[t] = __builtin_amdgcn_raw_buffer_load_b8(blk, F::k_scale(lane), 0, kPolicy);
+  r.vs[t] = __builtin_amdgcn_raw_buffer_load_b32(blk, F::v_scale(lane), 0, kPolicy);
 }
 
 __device__ __forceinline__ uint32_t lo_halves(uint32_t a, uint32_t b) {
@@ -64,7 +64,7 @@ __device__ __forceinline__ uint32_t v_pair(const uint32_t (&v)[Kv4<D>::kWords], 
   else return i & 1 ? kv4_pair<2 + (kS & 1)>(v[i >> 1], f) : kv4_pair<(kS & 1)>(v[i >> 1], f);
 }
 
-template <int D, bool kAppend, int kWaves>
+template <int D, bool kAppend, int kWaves, int kSets, int kPolicy>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void kv4_decode_kernel(Kv4AttnArgs a) {
   using F = Kv4<D>;
@@ -76,9 +76,8 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
   const int head = blockIdx.x - rg * a.num_kv_heads;
   const int run = rg * kWaves + wave;
   // the waves' partials at the end: outputs, statistics
-  __shared__ __attribute__((aligned(16))) uint8_t lds_o[kWaves * 16 * 4 * D];
-  __shared__ __attribute__((aligned(16))) uint8_t lds_s[kWaves * 16 * 4 * D / (D / 4)];
-  static_assert(sizeof(lds_s) == kWaves * 256, "16 bytes a row");
+  __shared__ __attribute__((aligned(16))) uint8_t lds_o[kWaves * kSets * 16 * 4 * D];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_s[kWaves * kSets * 16 * 16];
   __shared__ int open_unit[kWaves];  // the unit each wave leaves unfinished, or -1
 
   const bool live = run < R;
@@ -87,8 +86,10 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
   const int64_t slot0 = (int64_t)head * slots.count();
   const int G = a.group, Hkv = a.num_kv_heads;
   const int col = lane & 15, grp = lane >> 4;
-  const int tok = col / G;  // of the unit; the column's query head is col - tok * G of the kv head
-  const int64_t col_row = (int64_t)tok * a.num_q_heads + head * G + (col - tok * G);
+  // column `col` of set x is row 16 x + col of the unit: token tok[x], query head row - tok G of the group
+  int tok[kSets];
+#pragma unroll
+  for (int x = 0; x < kSets; ++x) tok[x] = (16 * x + col) / G;
 
   // Position in the sequence of the units' steps; all wave-uniform.
   struct Cursor {
@@ -135,8 +136,8 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
     flag_error |= (in && !ok0) || (second && !ok1);
     const int64_t b0 = ((int64_t)(ok0 ? pg[0] : 0) * Hkv + head) * F::kBlock;
     const int64_t b1 = ((int64_t)(ok1 ? pg[1] : 0) * Hkv + head) * F::kBlock;
-    kv4_load_page<D>(r, 0, block_rsrc(a.pool + b0, ok0 ? F::kBlock : 0), lane);
-    kv4_load_page<D>(r, 1, block_rsrc(a.pool + b1, ok1 ? F::kBlock : 0), lane);
+    kv4_load_page<D, kPolicy>(r, 0, block_rsrc(a.pool + b0, ok0 ? F::kBlock : 0), lane);
+    kv4_load_page<D, kPolicy>(r, 1, block_rsrc(a.pool + b1, ok1 ? F::kBlock : 0), lane);
     if constexpr (kAppend) {
       nw.page = -1;
       if (in && ld.step == ld.steps - 1) {
@@ -161,23 +162,35 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
     fetch_pages();
   };
 
-  bf16x8 qf[kC];
-  bool col_ok = false;
-  int64_t orow = 0;
-  auto load_q = [&]() {
-    col_ok = col < cu.tokens * G;
-    orow = (int64_t)cu.row_start * a.num_q_heads + col_row;
-#pragma unroll
-    for (int c = 0; c < kC; ++c)
-      qf[c] = as_bf16x8(col_ok ? load_u32x4(a.q + orow * D + (D / 4) * grp + 8 * c) : zero_u32x4());
+  bf16x8 qf[kSets][kC];
+  auto row_ok = [&](int x) { return 16 * x + col < cu.tokens * G; };
+  auto out_row = [&](int x) {
+    return ((int64_t)cu.row_start + tok[x]) * a.num_q_heads + head * G + (16 * x + col - tok[x] * G);
   };
-  f32x4 o[kJ];
-  float m_ref, l_part, l_exact;
-  auto reset = [&]() {
+  auto load_q = [&]() {
 #pragma unroll
-    for (int j = 0; j < kJ; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    m_ref = kNoMax;
-    l_part = l_exact = 0.0f;
+    for (int x = 0; x < kSets; ++x) {
+      const uint16_t* from = a.q + out_row(x) * D + (D / 4) * grp;
+#pragma unroll
+      for (int c = 0; c < kC; ++c) qf[x][c] = as_bf16x8(row_ok(x) ? load_u32x4(from + 8 * c) : zero_u32x4());
+    }
+  };
+  // The accumulators of a new unit are cleared where its first step raises the reference: set to zero
+  // at the last one's end they would be copied on every step, where that path joins the others.
+  f32x4 o[kSets][kJ];
+#pragma unroll
+  for (int x = 0; x < kSets; ++x)
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) o[x][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m_ref[kSets], l_part[kSets], l_exact[kSets];
+  bool fresh;
+  auto reset = [&]() {
+    fresh = true;
+#pragma unroll
+    for (int x = 0; x < kSets; ++x) {
+      m_ref[x] = kNoMax;
+      l_part[x] = l_exact[x] = 0.0f;
+    }
   };
 
   // The newest token takes the place of its slot in the operands (whatever the pool holds there)
@@ -256,53 +269,72 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
           else cur.v[t][i >> 1] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
         }
     }
-    f32x4 s[2];
+    f32x4 s[kSets][2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const float f = kv4_factor(cur.ks[t]);
-      s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int c = 0; c < kC; ++c) s[t] = mfma16(kv4_octet(cur.k[t][c], f), qf[c], s[t]);
+      for (int c = 0; c < kC; ++c) {
+        const bf16x8 kk = kv4_octet(cur.k[t][c], f);
+#pragma unroll
+        for (int x = 0; x < kSets; ++x)
+          s[x][t] = mfma16(kk, qf[x][c], c == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[x][t]);
+      }
     }
-    float mt = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[t][e] *= a.scale_log2;
     if (k + kDecodeStep > cu.prefix + 1) {  // keys that some token of the unit does not see
-      const int keys = cu.prefix + 1 + tok - k - 4 * grp;  // of this lane's, counted from its first
+#pragma unroll
+      for (int x = 0; x < kSets; ++x) {
+        const int keys = cu.prefix + 1 + tok[x] - k - 4 * grp;  // of this lane's, counted from its first
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[x][t][e] = 16 * t + e < keys ? s[x][t][e] : -INFINITY;
+      }
+    }
+    float mt[kSets];
+    bool raise = false;
+#pragma unroll
+    for (int x = 0; x < kSets; ++x) {
+      float m = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[t][e] = 16 * t + e < keys ? s[t][e] : -INFINITY;
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, s[x][t][e]);
+      m = fmaxf(m, xor_shfl(m, 16));
+      mt[x] = fmaxf(m, xor_shfl(m, 32)) * a.scale_log2;
+      raise |= mt[x] > m_ref[x] + kRescaleSlack;
     }
+    if (fresh || __any(raise)) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int x = 0; x < kSets; ++x) {
+        const float m_new = fmaxf(m_ref[x], mt[x]);
+        const float alpha = fast_exp2(m_ref[x] - m_new);
+        l_part[x] *= alpha;
+        l_exact[x] *= alpha;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mt = fmaxf(mt, s[t][e]);
-    mt = fmaxf(mt, xor_shfl(mt, 16));
-    mt = fmaxf(mt, xor_shfl(mt, 32));
-    if (__any(mt > m_ref + kRescaleSlack)) {
-      const float m_new = fmaxf(m_ref, mt);
-      const float alpha = fast_exp2(m_ref - m_new);
-      l_part *= alpha;
-      l_exact *= alpha;
+        for (int j = 0; j < kJ; ++j)
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) o[j] *= alpha;
-      m_ref = m_new;
-    }
-    u32x4 wp;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float p0 = fast_exp2(s[t][2 * e] - m_ref);
-        const float p1 = fast_exp2(s[t][2 * e + 1] - m_ref);
-        wp[2 * t + e] = pack_bf16x2(p0, p1);
-        l_part = add_bf16x2(wp[2 * t + e], l_part);
-        l_exact += p0 + p1;
+          for (int i = 0; i < 4; ++i) o[x][j][i] = fresh ? 0.0f : o[x][j][i] * alpha;
+        m_ref[x] = m_new;
       }
-    const bf16x8 pb = as_bf16x8(wp);
+      fresh = false;
+    }
+    bf16x8 pb[kSets];
+#pragma unroll
+    for (int x = 0; x < kSets; ++x) {
+      u32x4 wp;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float p0 = fast_exp2(s[x][t][2 * e] * a.scale_log2 - m_ref[x]);
+          const float p1 = fast_exp2(s[x][t][2 * e + 1] * a.scale_log2 - m_ref[x]);
+          wp[2 * t + e] = pack_bf16x2(p0, p1);
+          l_part[x] = add_bf16x2(wp[2 * t + e], l_part[x]);
+          if (a.lse) l_exact[x] += p0 + p1;
+        }
+      pb[x] = as_bf16x8(wp);
+    }
     float vf[2][4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -311,17 +343,20 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
     auto product = [&](auto tag) {
       constexpr int kS = decltype(tag)::value;
       if constexpr (kS < kJ / 2) {
-        uint32_t x[2][4];
+        uint32_t y[2][4];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[t][i] = v_pair<D, kS>(cur.v[t], i, vf[t][i]);
-        const u32x4 even = {lo_halves(x[0][0], x[0][1]), lo_halves(x[0][2], x[0][3]),
-                            lo_halves(x[1][0], x[1][1]), lo_halves(x[1][2], x[1][3])};
-        const u32x4 odd = {hi_halves(x[0][0], x[0][1]), hi_halves(x[0][2], x[0][3]),
-                           hi_halves(x[1][0], x[1][1]), hi_halves(x[1][2], x[1][3])};
-        o[2 * kS] = mfma16(as_bf16x8(even), pb, o[2 * kS]);
-        o[2 * kS + 1] = mfma16(as_bf16x8(odd), pb, o[2 * kS + 1]);
+          for (int i = 0; i < 4; ++i) y[t][i] = v_pair<D, kS>(cur.v[t], i, vf[t][i]);
+        const u32x4 even = {lo_halves(y[0][0], y[0][1]), lo_halves(y[0][2], y[0][3]),
+                            lo_halves(y[1][0], y[1][1]), lo_halves(y[1][2], y[1][3])};
+        const u32x4 odd = {hi_halves(y[0][0], y[0][1]), hi_halves(y[0][2], y[0][3]),
+                           hi_halves(y[1][0], y[1][1]), hi_halves(y[1][2], y[1][3])};
+#pragma unroll
+        for (int x = 0; x < kSets; ++x) {
+          o[x][2 * kS] = mfma16(as_bf16x8(even), pb[x], o[x][2 * kS]);
+          o[x][2 * kS + 1] = mfma16(as_bf16x8(odd), pb[x], o[x][2 * kS + 1]);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -335,11 +370,11 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
     v += xor_shfl(v, 16);
     return v + xor_shfl(v, 32);
   };
-  // Lane (col, grp) holds entries (D/4) grp + kJ i + j of its row as o[j][i]; four at a time:
-  // quad x is entries (D/4) grp + 4 x.
-  auto quad = [&](int x) {
-    const int i = 4 * x / kJ, j = 4 * x % kJ;
-    return f32x4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
+  // Lane (col, grp) holds entries (D/4) grp + kJ i + j of its row of set x as o[x][j][i]; four at a
+  // time: quad y is entries (D/4) grp + 4 y.
+  auto quad = [&](int x, int y) {
+    const int i = 4 * y / kJ, j = 4 * y % kJ;
+    return f32x4{o[x][j][i], o[x][j + 1][i], o[x][j + 2][i], o[x][j + 3][i]};
   };
   constexpr int kQuads = D / 16;
 
@@ -350,16 +385,19 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
   // The unit whose last step was just computed.
   auto unit_end = [&]() {
     if (begin == 0) {  // all of it in this wave: its rows are final
-      const float inv = 1.0f / sum_cols(l_part), lx = sum_cols(l_exact);
-      if (col_ok) {
-        uint16_t* to = a.out + orow * D + (D / 4) * grp;
 #pragma unroll
-        for (int x = 0; x < kQuads; x += 2) {
-          const f32x4 q0 = quad(x), q1 = quad(x + 1);
-          store_u32x4(to + 4 * x, u32x4{pack_bf16x2(q0[0] * inv, q0[1] * inv), pack_bf16x2(q0[2] * inv, q0[3] * inv),
+      for (int x = 0; x < kSets; ++x) {
+        const float inv = 1.0f / sum_cols(l_part[x]), lx = sum_cols(l_exact[x]);
+        if (!row_ok(x)) continue;
+        const int64_t row = out_row(x);
+        uint16_t* to = a.out + row * D + (D / 4) * grp;
+#pragma unroll
+        for (int y = 0; y < kQuads; y += 2) {
+          const f32x4 q0 = quad(x, y), q1 = quad(x, y + 1);
+          store_u32x4(to + 4 * y, u32x4{pack_bf16x2(q0[0] * inv, q0[1] * inv), pack_bf16x2(q0[2] * inv, q0[3] * inv),
                                         pack_bf16x2(q1[0] * inv, q1[1] * inv), pack_bf16x2(q1[2] * inv, q1[3] * inv)});
         }
-        if (a.lse && grp == 0) a.lse[orow] = (m_ref + __log2f(lx)) * kLn2;
+        if (a.lse && grp == 0) a.lse[row] = (m_ref[x] + __log2f(lx)) * kLn2;
       }
     } else if (cu.steps - begin == a.steps) {  // it took the whole run: like an unfinished one
       has_final = true;
@@ -368,15 +406,18 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
       has_flush = true;
       flush_unit = cu.unit, flush_row = cu.row_start, flush_tokens = cu.tokens;
       flush = stream_unit(run, begin, cu.steps - begin, cu.steps, a.steps);
-      const float l = sum_cols(l_part), lx = sum_cols(l_exact);
-      if (col < a.cols) {
-        const int64_t slot = slot0 + slots.ended(run, cu.unit);
-        float* po = a.part_o + slot * a.cols * D;
+      const int64_t slot = slot0 + slots.ended(run, cu.unit);
+      float* po = a.part_o + slot * a.cols * D;
 #pragma unroll
-        for (int x = 0; x < kQuads; ++x)
-          store_f32x4_device(po, a.cols * D * 4, 4 * (col * D + (D / 4) * grp + 4 * x), quad(x));
+      for (int x = 0; x < kSets; ++x) {
+        const float l = sum_cols(l_part[x]), lx = sum_cols(l_exact[x]);
+        const int row = 16 * x + col;
+        if (row >= a.cols) continue;
+#pragma unroll
+        for (int y = 0; y < kQuads; ++y)
+          store_f32x4_device(po, a.cols * D * 4, 4 * (row * D + (D / 4) * grp + 4 * y), quad(x, y));
         if (grp == 0)
-          store_f32x4_device(a.part_ml + slot * a.cols * 4, a.cols * 16, 16 * col, f32x4{m_ref, l, lx, 0.0f});
+          store_f32x4_device(a.part_ml + slot * a.cols * 4, a.cols * 16, 16 * row, f32x4{m_ref[x], l, lx, 0.0f});
       }
     }
     begin = 0;
@@ -403,11 +444,11 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
   reset();
   fetch_pages();
   if (n > 0) {
-    Kv4Regs<D> r0, r1, r2;
-    NewRow n0, n1, n2;
+    Kv4Regs<D> r0, r1;
+    NewRow n0, n1;
     load_q();
     // every load is issued on straight-line code (past the run's end, loads of nothing), so that a
-    // step's wait leaves the next two in flight.  The loop has one exit: with one behind each
+    // step's wait leaves the next in flight.  The loop has one exit: with one behind each
     // step the accumulators got registers of their own per copy of the step (60 more a copy).
     auto trip = [&](Kv4Regs<D>& next, NewRow& next_new, Kv4Regs<D>& r, NewRow& nw) {
       issue(next, next_new);
@@ -415,26 +456,28 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
       if (done < n) process(r, nw);
     };
     issue(r0, n0);
-    issue(r1, n1);
     do {
-      trip(r2, n2, r0, n0);
+      trip(r1, n1, r0, n0);
       trip(r0, n0, r1, n1);
-      trip(r1, n1, r2, n2);
     } while (done < n);
     has_final |= cu.step > 0 && cu.step < cu.steps;
   }
   if (flag_error && lane == 0) atomicOr(a.error_flags, 1);
 
   // ---- parts of cut units (decode_runs.h) ---------------------------------------------------
-  uint8_t* const my_o = lds_o + wave * 64 * D;
-  uint8_t* const my_s = lds_s + wave * 256;
+  constexpr int kStrideO = kSets * 64 * D, kStrideS = kSets * 256;  // a wave's rows and statistics
+  uint8_t* const my_o = lds_o + wave * kStrideO;
+  uint8_t* const my_s = lds_s + wave * kStrideS;
   if (has_final) {
-    const float l = sum_cols(l_part), lx = sum_cols(l_exact);
-    // row `col` of the wave's partial: 16-byte granule g at g ^ col
 #pragma unroll
-    for (int x = 0; x < kQuads; ++x)
-      *reinterpret_cast<f32x4*>(my_o + 4 * D * col + 16 * (((D / 16) * grp + x) ^ col)) = quad(x);
-    if (grp == 0) *reinterpret_cast<f32x4*>(my_s + 16 * col) = f32x4{m_ref, l, lx, 0.0f};
+    for (int x = 0; x < kSets; ++x) {
+      const float l = sum_cols(l_part[x]), lx = sum_cols(l_exact[x]);
+      // row 16 x + col of the wave's partial: 16-byte granule g at g ^ col
+#pragma unroll
+      for (int y = 0; y < kQuads; ++y)
+        *reinterpret_cast<f32x4*>(my_o + 4 * D * (16 * x + col) + 16 * (((D / 16) * grp + y) ^ col)) = quad(x, y);
+      if (grp == 0) *reinterpret_cast<f32x4*>(my_s + 16 * (16 * x + col)) = f32x4{m_ref[x], l, lx, 0.0f};
+    }
   }
   if (lane == 0) open_unit[wave] = has_final ? cu.unit : -1;
   __syncthreads();
@@ -461,38 +504,55 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
   while (wave + len < kWaves && left_open(wave + len) == cu.unit) ++len;
   const StreamUnit u = stream_unit(run, begin, cu.step - begin, cu.steps, a.steps);
   const bool whole = !u.ends_inside && u.n == len;  // the unit lies inside this workgroup
-  parts_of(cu.row_start, cu.tokens).close(my_o, my_s, 64 * D, 256, len, whole, u, run, cu.unit);
+  parts_of(cu.row_start, cu.tokens).close(my_o, my_s, kStrideO, kStrideS, len, whole, u, run, cu.unit);
 }
 
-template <int D, bool kAppend>
+template <int D, bool kAppend, int kSets, int kPolicy>
 hipError_t launch_kv4(const Kv4AttnArgs& a, hipStream_t stream) {
   const int waves = kv4_waves((int64_t)a.num_runs * a.num_kv_heads);
   const dim3 blocks(kv4_groups(a.num_runs, a.num_kv_heads));
   if (waves == kKv4Big)
-    hipLaunchKernelGGL((kv4_decode_kernel<D, kAppend, kKv4Big>), blocks, dim3(kKv4Big * 64), 0, stream, a);
+    hipLaunchKernelGGL((kv4_decode_kernel<D, kAppend, kKv4Big, kSets, kPolicy>), blocks, dim3(kKv4Big * 64), 0, stream,
+                       a);
   else
-    hipLaunchKernelGGL((kv4_decode_kernel<D, kAppend, kKv4Small>), blocks, dim3(kKv4Small * 64), 0, stream, a);
+    hipLaunchKernelGGL((kv4_decode_kernel<D, kAppend, kKv4Small, kSets, kPolicy>), blocks, dim3(kKv4Small * 64), 0,
+                       stream, a);
   return hipGetLastError();
 }
 
 // Every variant is instantiated explicitly (see attn_decode.hip).
-template __global__ void kv4_decode_kernel<128, false, kKv4Big>(Kv4AttnArgs);
-template __global__ void kv4_decode_kernel<128, false, kKv4Small>(Kv4AttnArgs);
-template __global__ void kv4_decode_kernel<128, true, kKv4Big>(Kv4AttnArgs);
-template __global__ void kv4_decode_kernel<128, true, kKv4Small>(Kv4AttnArgs);
-template __global__ void kv4_decode_kernel<64, false, kKv4Big>(Kv4AttnArgs);
-template __global__ void kv4_decode_kernel<64, false, kKv4Small>(Kv4AttnArgs);
-template __global__ void kv4_decode_kernel<64, true, kKv4Big>(Kv4AttnArgs);
-template __global__ void kv4_decode_kernel<64, true, kKv4Small>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, false, kKv4Big, 1, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, false, kKv4Small, 1, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, true, kKv4Big, 1, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, true, kKv4Small, 1, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, false, kKv4Big, 2, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, false, kKv4Small, 2, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, false, kKv4Big, 2, kSharedPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<128, false, kKv4Small, 2, kSharedPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, false, kKv4Big, 1, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, false, kKv4Small, 1, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, true, kKv4Big, 1, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, true, kKv4Small, 1, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, false, kKv4Big, 2, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, false, kKv4Small, 2, kStreamPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, false, kKv4Big, 2, kSharedPolicy>(Kv4AttnArgs);
+template __global__ void kv4_decode_kernel<64, false, kKv4Small, 2, kSharedPolicy>(Kv4AttnArgs);
+
+// One set of columns where every unit has at most 16 rows.  Codes that one unit alone reads are streamed
+// past the caches (256 tasks' decode 384 us, 429 without); those that the next unit of their task reads
+// again are not.
+template <int D>
+hipError_t launch_kv4(const Kv4AttnArgs& a, hipStream_t stream) {
+  if (a.k_new) return launch_kv4<D, true, 1, kStreamPolicy>(a, stream);
+  if (a.cols <= 16) return launch_kv4<D, false, 1, kStreamPolicy>(a, stream);
+  return a.reread ? launch_kv4<D, false, 2, kSharedPolicy>(a, stream) : launch_kv4<D, false, 2, kStreamPolicy>(a, stream);
+}
 
 }  // namespace kern
 
 hipError_t launch_kv4_decode(const Kv4AttnArgs& a, int head_dim, hipStream_t stream) {
-  const bool append = a.k_new != nullptr;
-  if (head_dim == 128)
-    return append ? kern::launch_kv4<128, true>(a, stream) : kern::launch_kv4<128, false>(a, stream);
-  if (head_dim == 64)
-    return append ? kern::launch_kv4<64, true>(a, stream) : kern::launch_kv4<64, false>(a, stream);
+  if (head_dim == 128) return kern::launch_kv4<128>(a, stream);
+  if (head_dim == 64) return kern::launch_kv4<64>(a, stream);
   return hipErrorInvalidValue;
 }
 

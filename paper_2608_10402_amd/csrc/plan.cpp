@@ -1006,7 +1006,12 @@ constexpr int64_t kMassBlockCost = 2;  // reading a block and its sums, in trips
 constexpr int64_t kKv4StageBytes = (int64_t)1 << 30;
 constexpr int32_t kKv4StagePages = 16;  // most pages of a staging item
 constexpr int64_t kKv4StageItems = 1024;  // items that a short call is cut into
-constexpr int32_t kKv4DirectTokens = 16;
+// An extend reads the codes once per unit, or unpacks its tasks' pages and lets the bf16 kernel read
+// them.  Where the units that a key is read for are fewer than this, on average, the first is faster.
+// Call us, codes and unpacked, 32 tasks of 2k-16k keys: 28 / 4 heads, d = 128, 8 tokens (2 units) 73 and
+// 290, 24 (6) 179 and 310, 48 (12) 326 and 377, 64 (16) 426 and 394; 32 / 8 heads, 64 tokens (8) 463 and
+// 636; 32 / 2, d = 64, 8 tokens (4) 58 and 75, 16 (8) 97 and 90, 32 (16) 174 and 128.
+constexpr int64_t kKv4DirectUnits = 12, kKv4DirectUnits64 = 7;
 
 // Appends `n` records to a plan's blob region at `off` (grown to its end) and returns the end.
 template <class T>
@@ -1068,12 +1073,14 @@ int make_plan_kv4_units(int op, int32_t num_tasks, const int32_t* lens_a, const 
   std::vector<TaskDesc> units;
   int64_t total = 0, longest = 0, rows = 0;
   int32_t widest = 1;
+  bool reread = false;
   for (int32_t b = 0; b < num_tasks; ++b) {
     int32_t p = 0, e = 0;
     rc = task_lengths(op == TIDE_OP_KV4_DECODE ? TIDE_OP_DECODE : TIDE_OP_EXTEND, b, lens_a, lens_b, &p, &e);
     if (rc != TIDE_OK) return rc;
     if (rows + e > INT32_MAX) return TIDE_ERR_INVALID_ARG;
     if (bt_stride >= 0 && ceil_div((int64_t)p + e, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
+    reread |= e > most;
     for (int32_t t = 0; t < e; t += most) {
       const int32_t n = std::min(most, e - t);
       units.push_back(TaskDesc{(int32_t)rows + t, p + t, n, b});
@@ -1084,12 +1091,13 @@ int make_plan_kv4_units(int op, int32_t num_tasks, const int32_t* lens_a, const 
     }
     rows += e;
   }
-  if (units.size() > (size_t)INT32_MAX / kMaxGroup) return TIDE_ERR_INVALID_ARG;
+  if (units.size() > (size_t)INT32_MAX / kKv4Cols) return TIDE_ERR_INVALID_ARG;
   *plan = Plan();
   plan->op = op;
   plan->num_tasks = (int32_t)units.size();
   plan->total_rows = (int32_t)rows;
   plan->tokens_per_item = widest;
+  plan->reread = reread;
   if (units.empty()) {
     plan->total_bytes = plan->upload_bytes = sizeof(WsHeader);
     return TIDE_OK;
@@ -1140,8 +1148,10 @@ int make_plan_kv4_extend(int32_t num_tasks, const int32_t* prefix_lens, const in
   int rc = check_dims(&dims);
   if (rc != TIDE_OK) return rc;
   *plan = Kv4ExtendPlan();
-  int32_t longest = 0;
+  const int32_t most = kKv4Cols / (dims.num_q_heads / dims.num_kv_heads);  // tokens of a unit
+  const int64_t direct = dims.head_dim == 64 ? kKv4DirectUnits64 : kKv4DirectUnits;
   int64_t rows = 0;
+  double keys = 0.0, reads = 0.0;
   for (int32_t b = 0; b < num_tasks; ++b) {
     int32_t p = 0, e = 0;
     rc = task_lengths(TIDE_OP_EXTEND, b, prefix_lens, extend_lens, &p, &e);
@@ -1149,9 +1159,11 @@ int make_plan_kv4_extend(int32_t num_tasks, const int32_t* prefix_lens, const in
     rows += e;
     if (rows > INT32_MAX) return TIDE_ERR_INVALID_ARG;
     if (bt_stride >= 0 && ceil_div((int64_t)p + e, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
-    longest = std::max(longest, e);
+    if (e == 0) continue;
+    keys += (double)p + e;
+    reads += ((double)p + e) * ceil_div(e, most);
   }
-  if (longest <= kKv4DirectTokens) {
+  if (reads <= direct * keys) {
     plan->by_units = true;
     rc = make_plan_kv4_units(TIDE_OP_KV4_EXTEND, num_tasks, prefix_lens, extend_lens, dims, bt_stride, build_blob,
                              &plan->units);

@@ -48,6 +48,7 @@ struct Plan {
   // extend: tokens per work item and waves per workgroup
   int32_t tokens_per_item = 0;
   int32_t waves = 0;
+  bool reread = false;    // 4-bit attention: some task has several units
   bool one_trip = false;  // attention mass: no task has over 16 query rows a kv head
   // extend: passes over the blocks that the search for the chunk length made
   int32_t search_passes = 0;

@@ -310,8 +310,9 @@ struct StreamArgs {
 // Bytes of one (page, kv head) block: K codes, V codes, K scales, V scales (kv4.h).
 TIDE_HD constexpr int kv4_block_bytes(int head_dim) { return 17 * head_dim; }
 
-// Query rows (tokens x heads of a kv head) of one attention unit: the columns of a 16-wide MFMA.
-constexpr int kKv4Cols = 16;
+// Query rows (tokens x heads of a kv head) of one attention unit: the columns of one 16-wide MFMA or
+// two.
+constexpr int kKv4Cols = 32;
 
 // Waves per workgroup of such attention, and workgroups, as stream_waves and stream_groups.
 TIDE_HD inline int32_t kv4_waves(int64_t items) { return items > 256 ? 8 : 4; }
@@ -406,6 +407,7 @@ struct Kv4AttnArgs {
   const TaskDesc* units;
   const Kv4Run* runs;
   int32_t num_units;
+  bool reread;  // some task has several units
   float* part_o;   // [Hkv][slots][cols][d]
   float* part_ml;  // [Hkv][slots][cols][4]
   uint64_t* flags;
