@@ -119,7 +119,9 @@ def test_values_at_the_edges_of_the_format(d):
 DECODE = [  # hq, hkv, d, lens
     (1, 1, 128, [1]), (8, 2, 64, [1, 2, 15, 16, 17, 31, 32, 33, 47, 48, 49]), (7, 1, 128, [100, 7, 1000]),
     (28, 4, 128, [300, 1999, 45]), (16, 1, 64, [513]), (16, 1, 128, [2048, 5]), (32, 8, 128, list(range(1, 130, 9))),
-    (4, 4, 64, [4097]), (32, 2, 64, [6000]), (64, 8, 128, [777, 1]), (28, 4, 128, [40] * 70)]
+    (4, 4, 64, [4097]), (32, 2, 64, [6000]), (64, 8, 128, [777, 1]), (28, 4, 128, [40] * 70),
+    (2500, 2500, 64, [70, 5]),                              # more kv heads than waves
+    (8, 4, 64, [1 + 37 * i % 60 for i in range(1500)])]     # more tasks than runs
 
 
 @pytest.mark.parametrize("hq,hkv,d,lens", DECODE)
@@ -156,6 +158,7 @@ EXTEND = [  # hq, hkv, d, prefix, extend
     (28, 4, 128, [37, 0, 200], [1, 2, 3]),            # few tokens: the codes themselves
     (32, 8, 128, [1000, 15, 16, 0], [8, 5, 0, 1]),
     (16, 1, 64, [300], [7]), (3, 3, 64, [64, 1], [16, 16]), (1, 1, 128, [5], [16]),
+    (16, 1, 128, [64, 7], [2, 1]), (28, 4, 128, [300, 33], [48, 2]), (32, 2, 64, [500, 70], [12, 5]),  # several units
     (28, 4, 128, [100, 0, 411], [130, 17, 1]),        # staged
     (8, 2, 64, [37, 250, 0], [5, 0, 200]), (16, 1, 128, [0], [65]), (4, 4, 128, [90], [300])]
 
@@ -216,7 +219,7 @@ def test_bad_page_ids_are_reported_and_never_read(call, monkeypatch):
         if call == "extend_few":
             return f.kv.extend(q[:4], f.lens - 2, [2, 2])
         if call == "extend":
-            return f.kv.extend(q[:60], f.lens - 30, [30, 30])
+            return f.kv.extend(q[:140], f.lens - np.array([90, 50], np.int32), [90, 50])  # (unpacked pages)
         if call == "append":
             return f.kv.append(*new, [0, 0], f.lens)
         return f.kv.unpack([0, 0], f.lens)
@@ -270,13 +273,17 @@ def test_offsets_past_32_bits():
     check(host(out), None, R.attention(q[:1], k4, v4, 39, 128 ** -0.5))
 
 
-def test_other_stream_and_graph_replays():
+@pytest.mark.parametrize("unpacked", [False, True])
+def test_other_stream_and_graph_replays(unpacked):
     """Captured calls, replayed between eager ones on other data, against the eager results."""
     f = Filled(31, [200, 77, 1], 28, 4, 128)
     n = 3
     q, k, v = rows_to_dev(f.queries(n)), *(rows_to_dev(R.bf16(f.rng.standard_normal((n, 4, 128)))) for _ in range(2))
-    qx = rows_to_dev(f.queries(40 + 30))
-    ext = (f.lens - np.array([40, 30, 0], np.int32), [40, 30, 0])
+    new = [150, 70, 0] if unpacked else [40, 30, 0]
+    qx = rows_to_dev(f.queries(sum(new)))
+    ext = (f.lens - np.array(new, np.int32), new)
+    info = tide.tide_plan_info_get(tide.TIDE_OP_KV4_EXTEND, *ext, f.kv.dims)
+    assert (info["run_steps"] == 0) == unpacked
     pool = f.kv.pool.clone()
     want = f.kv.decode_append(q, k, v, f.lens).clone()
     wantx = f.kv.extend(qx, *ext).clone()
