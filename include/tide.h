@@ -21,6 +21,8 @@
  *     tide_decode_append_attn tide_kv_append of one token per task + tide_decode_attn
  *   and decode for GRPO groups whose trajectories share a prompt prefix:
  *     tide_decode_attn_shared tide_decode_attn, reading each shared prefix once per group
+ *   The same steps over a cache held in 4 bits (tide_kv4_*), and the eviction of the positions that a
+ *   task's queries attended to least (tide_attn_mass, tide_kv_evict).
  *
  *   The attention itself is standard scaled dot-product attention (Vaswani et al.,
  *   2017), which the paper uses but does not restate: for a query row at absolute
@@ -383,7 +385,8 @@ TIDE_API int tide_kv4_decode_append_attn(const void* q, const void* k_new, const
  * tide_extend_attn over a 4-bit pool (the new tokens appended before).  A call of a few tokens a task
  * reads the codes themselves; a larger one unpacks its tasks' pages into the workspace and attends
  * over those.  Workspace: TIDE_OP_KV4_EXTEND, up to 1 GiB of unpacked pages (one task's
- * if that is more).
+ * if that is more).  A new token's V that is NaN or infinite may reach every row of its task in the call,
+ * those before it too.
  */
 TIDE_API int tide_kv4_extend_attn(const void* q, const void* kv4_pool, int64_t num_pages,
                          const int32_t* block_table, int32_t bt_stride, int32_t num_tasks,
@@ -406,6 +409,7 @@ TIDE_API int tide_kv4_extend_attn(const void* q, const void* kv4_pool, int64_t n
  *                + sum over new tokens j with prefix + j >= p, query heads h of g:
  *                      exp(sm_scale * <q_jh, k_pg> - lse_jh)
  *   q, lse        as the attention call took and returned them, packed by extend_lens
+ *                 (a row whose lse is not finite reaches the keys that it sees and no other)
  *   counted_lens  positions whose sums are carried on (at most prefix + extend); NULL: prefix_lens,
  *                 so that the new tokens' own sums start at 0
  * Tokens of which only the last w are to count: prefix + extend - w and w, with counted_lens = the
@@ -425,8 +429,12 @@ TIDE_API int tide_kv4_attn_mass(const void* q, const float* lse, const void* kv4
                        const int32_t* counted_lens, const tide_dims* dims, float* mass_pool,
                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* Longest context of an eviction. */
+#define TIDE_EVICT_MAX_LEN 0x7FF00000
+
 /*
- * Cuts each task's context from kv_lens[b] to keep_lens[b] <= kv_lens[b] positions.  Every KV head
+ * Cuts each task's context from kv_lens[b] <= TIDE_EVICT_MAX_LEN (TIDE_ERR_INVALID_ARG beyond) to
+ * keep_lens[b] <= kv_lens[b] positions.  Every KV head
  * keeps the last recent_lens[b] <= keep_lens[b] positions (NULL: none) and, of those before, the
  * ones with the largest sums (equal sums: the earlier position; NaN counts as the least), and moves
  * K, V and sums of what it keeps, in order, to positions 0 .. keep_lens[b] - 1.  The heads keep

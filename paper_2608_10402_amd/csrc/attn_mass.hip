@@ -87,7 +87,7 @@ void attn_mass_kernel(MassArgs a) {
     c.prefix = t[1];
     c.extend = t[2];
     c.counted = t[3];
-    c.blocks = c.extend > 0 ? (c.prefix + c.extend + 63) / 64 : 0;
+    c.blocks = c.extend > 0 ? (c.prefix + c.extend - 1) / kMassKeys + 1 : 0;
   };
   auto next_block = [&](Cursor& c, bool more) {  // more: there is one (it is not looked for otherwise)
     if (++c.block < c.blocks || !more) return;
@@ -115,12 +115,13 @@ void attn_mass_kernel(MassArgs a) {
     if (first_h >= G) first_h -= G, ++first;
   };
   auto token_of = [&](int r) { return (int)(__umul24(first_h + r, per_group) >> 16); };  // of row r, from `first`
-  // row r's place behind the first token's first query head, in rows
+  // Row r's place behind the first token's first query head, in rows.  In place of rows past the task's last
+  // that one is read: zeros would make NaN of a key that holds infinities, whose scores with the task's
+  // own rows may all be -inf.
   auto place_of = [&](int r) {
-    const int t = token_of(r);
-    return __umul24(t, a.num_q_heads - G) + (uint32_t)(first_h + r);
+    const int i = min(first_h + r, G * min(cu.extend - first, 32) - 1);
+    return __umul24(__umul24(i, per_group) >> 16, a.num_q_heads - G) + (uint32_t)i;
   };
-  // Rows past the task's last lie past the buffers' ends: zeros, no memory access.
   bf16x8 q[kC];
   float lse = 0.0f;
   auto load_rows = [&]() {
@@ -249,9 +250,9 @@ void attn_mass_kernel(MassArgs a) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
       const int row_tok = first + token_of(col);
-      const float bias = row_tok < cu.extend ? lse : INFINITY;  // no row: no weight
+      float bias = row_tok < cu.extend ? lse : INFINITY;  // no row: no weight
       const int seen = cu.prefix + row_tok + 1 - kb - 4 * grp;  // keys that the row sees, from this lane's first
-      const bool partial = kb + kMassKeys > cu.prefix + first + 1;
+      const bool partial = kb > cu.prefix + first + 1 - kMassKeys;
       if constexpr (!kOneTrip) next_rows();
       f32x4 s[4];
 #pragma unroll
@@ -261,9 +262,18 @@ void attn_mass_kernel(MassArgs a) {
         for (int c = 0; c < kC; ++c) s[t] = mfma16(kk[t][c], q[c], s[t]);
       }
       if (partial) {
+        auto hidden = [&](int i) { return 16 * (i >> 2) + (i & 3) >= seen; };
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (16 * (i >> 2) + (i & 3) >= seen) s[i >> 2][i & 3] = -INFINITY;
+          if (hidden(i)) s[i >> 2][i & 3] = -INFINITY;
+        // a log-sum-exp that would turn hidden keys' weights into NaN goes into the others' scores
+        const bool odd = !(bias > -INFINITY);
+        if (__any(odd)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (odd && !hidden(i)) s[i >> 2][i & 3] -= bias;
+          bias = odd ? 0.0f : bias;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[i] += fast_exp2(s[i >> 2][i & 3] * a.scale_log2 - bias);

@@ -102,12 +102,12 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
     c.prefix = u[1];
     c.tokens = u[2];
     c.table = a.block_table + (int64_t)u[3] * a.bt_stride;
-    c.steps = (c.prefix + c.tokens + kDecodeStep - 1) / kDecodeStep;
+    c.steps = (c.prefix + c.tokens - 1) / kDecodeStep + 1;
   };
   const const_run* it = (const const_run*)(a.runs + (live ? run : 0));
   Cursor ld = {it->unit, it->step, 0, it->desc.prefix, it->desc.extend, it->desc.row_start,
                a.block_table + (int64_t)it->desc.aux * a.bt_stride};
-  ld.steps = (ld.prefix + ld.tokens + kDecodeStep - 1) / kDecodeStep;
+  ld.steps = (ld.prefix + ld.tokens - 1) / kDecodeStep + 1;
   Cursor cu = ld;
 
   // Loads of the load cursor's step, through zero-length buffers (zeros, no memory access) past
@@ -281,7 +281,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
           s[x][t] = mfma16(kk, qf[x][c], c == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[x][t]);
       }
     }
-    if (k + kDecodeStep > cu.prefix + 1) {  // keys that some token of the unit does not see
+    if (k > cu.prefix + 1 - kDecodeStep) {  // keys that some token of the unit does not see
 #pragma unroll
       for (int x = 0; x < kSets; ++x) {
         const int keys = cu.prefix + 1 + tok[x] - k - 4 * grp;  // of this lane's, counted from its first

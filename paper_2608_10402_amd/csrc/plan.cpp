@@ -1316,7 +1316,8 @@ int make_plan_evict(int32_t num_tasks, const int32_t* kv_lens, const int32_t* ke
   int32_t longest = 0;
   for (int32_t b = 0; b < num_tasks; ++b) {
     const int32_t n = kv_lens[b], k = keep_lens[b], r = recent ? recent[b] : 0;
-    if (n < 0 || k < 0 || k > n || r < 0 || r > k) return TIDE_ERR_INVALID_ARG;
+    // (the kernels' positions stay in 31 bits, those of the chunks ahead too)
+    if (n < 0 || n > TIDE_EVICT_MAX_LEN || k < 0 || k > n || r < 0 || r > k) return TIDE_ERR_INVALID_ARG;
     if (bt_stride >= 0 && ceil_div(n, kPage) > bt_stride) return TIDE_ERR_CAPACITY;
     if (new_stride >= 0 && ceil_div(k, kPage) > new_stride) return TIDE_ERR_CAPACITY;
     if (k > 0) tasks.push_back(EvictTask{b, n, k, r, (int32_t)kept, {0, 0, 0}});

@@ -138,6 +138,13 @@ def test_workspace_sizes():
         size(tide.TIDE_OP_KV_EVICT, [10], [11])
 
 
+def test_longest_eviction():
+    most = 0x7FF00000  # TIDE_EVICT_MAX_LEN
+    assert size(tide.TIDE_OP_KV_EVICT, [most], [5]) > 0
+    with pytest.raises(tide.TideError):
+        size(tide.TIDE_OP_KV_EVICT, [most + 1], [5])
+
+
 def test_plan_info_of_the_4_bit_attention():
     info = tide.tide_plan_info_get(tide.TIDE_OP_KV4_DECODE, [100, 2000], None, GOOD)
     assert info["num_items"] % 4 == 0 and info["run_steps"] >= 1

@@ -104,6 +104,35 @@ def test_mass_ignores_what_lies_past_the_context(bits):
         assert np.abs(mine.sum((0, 2)) - e * 4).max() < 1e-4  # 12 rows of weights, each 1 within 1e-5
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("prefix,extend,bad", [(35, 5, 2), (61, 9, 3), (70, 30, 7), (0, 1, 0)])
+def test_mass_of_rows_that_are_not_numbers(prefix, extend, bad, bits):
+    """A row whose log-sum-exp is NaN or -inf reaches the keys that it sees, of its kv head, and no other; a
+    key that scores -inf with every row gets nothing."""
+    c = Cache(extend, [prefix + extend], 12, 2, 64, bits)
+    q = np.abs(c.rng.standard_normal((extend, 12, 64))) + 2.0 ** -6
+    lse = np.full((extend, 12), 4.0, np.float32)
+    lost = prefix + extend - 1  # (a key of the 4-bit cache holds no infinity)
+    if bits == 16:
+        c.kv.k_pool[int(c.table[0, lost // PAGE]), 1, lost % PAGE] = -np.inf
+    want = c.kv.new_mass()
+    c.kv.attn_mass(rows_to_dev(q), torch.from_numpy(lse).cuda(), [prefix], [extend], want)
+    pos = np.arange(prefix + extend)
+    page, slot = c.table[0][pos // PAGE], pos % PAGE
+    want = host(want)[page, :, slot]
+    assert np.isfinite(want).all()
+    if bits == 16:
+        assert want[lost, 1] == 0 and want[lost, 0] > 0
+    for value in (np.nan, -np.inf):
+        lse[bad, :6] = value  # kv head 0
+        mass = c.kv.new_mass()
+        c.kv.attn_mass(rows_to_dev(q), torch.from_numpy(lse).cuda(), [prefix], [extend], mass)
+        got = host(mass)[page, :, slot]
+        reached = pos <= prefix + bad
+        assert not np.isfinite(got[reached, 0]).any()
+        assert np.array_equal(got[~reached, 0], want[~reached, 0]) and np.array_equal(got[:, 1], want[:, 1])
+
+
 def check_evict(c, mass0, keep, recent, new_table=None, give_kept=True):
     """Evicts and compares pools, sums and kept positions with the definition, every slot."""
     mass = torch.from_numpy(mass0.copy()).cuda()
@@ -349,3 +378,39 @@ def test_graph_replays():
         c.kv.decode(q, c.lens, lse=lse)
         g.replay()
         assert torch.equal(mass, want_mass) and torch.equal(kept, want_kept) and torch.equal(c.kv.pool, want_pool), i
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_calls_on_two_streams_at_once(bits):
+    """Two caches, each with a workspace and a stream of its own, in turn and without waits between."""
+    caches = [Cache(7 + i, [400 + 90 * i, 33, 128], 16, 4, 128, bits) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in caches]
+    qs = [rows_to_dev(c.rng.standard_normal((3, 16, 128))) for c in caches]
+    keep = np.array([200, 20, 128], np.int32)
+
+    def step(c, q, mass):
+        """Decode, sums, eviction; returns what they wrote."""
+        lse = torch.empty((3, 16), device="cuda")
+        out = c.kv.decode(q, c.lens, lse=lse)
+        c.kv.attn_mass(q, lse, c.lens - 1, [1, 1, 1], mass)
+        return out, lse, mass.clone(), c.kv.evict(mass, c.lens, keep, recent_lens=[4, 4, 4])
+
+    def pools(c):
+        return [c.kv.pool] if bits == 4 else [c.kv.k_pool, c.kv.v_pool]
+
+    start = [[p.clone() for p in pools(c)] for c in caches]
+    want = [step(c, q, c.mass()) + tuple(p.clone() for p in pools(c)) for c, q in zip(caches, qs)]
+    for turn in range(10):
+        for c, p in zip(caches, start):
+            for a, b in zip(pools(c), p):
+                a.copy_(b)
+        sums = [c.mass() for c in caches]
+        torch.cuda.synchronize()
+        got = []
+        for c, q, m, s in zip(caches, qs, sums, streams):
+            with torch.cuda.stream(s):
+                got.append(step(c, q, m))
+        torch.cuda.synchronize()
+        for c, g, w in zip(caches, got, want):
+            for x, y in zip(g + tuple(pools(c)), w):
+                assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), turn
