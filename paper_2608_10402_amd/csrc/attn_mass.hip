@@ -10,11 +10,18 @@
 // same bits.  Scores, weights and sums are fp32.
 //
 // The blocks of all tasks, laid end to end, are cut into runs of equal cost (rows and reads), and
-// one wave takes a run of one kv head, the next block's loads behind the last rows of one.  Query rows pass through a wave's own 4 KB of LDS, whole
-// rows at a time, the next 16 on their way while 16 are used: as operands straight from memory, 64
-// lanes read 64 separate pieces, which kept the L1 busy for 73% of a call of 43 rows x 7 heads.
-// Where 16 rows are all of every task's (kOneTrip: decode steps), they are read as operands, once a
-// task, since the compiler lets every read of LDS wait for the K loads in flight, too.
+// one wave takes a run of one kv head, the next block's loads behind the last rows of one.
+// Query rows pass through a wave's own 4 KB of LDS, whole rows at a time, the next 16 on their way
+// while 16 are used: as operands straight from memory, 64 lanes read 64 separate pieces, which
+// kept the L1 busy for 73% of a call of 43 rows x 7 heads.  Where 16 rows are all of every task's
+// (kOneTrip: decode steps), they are read as operands, once a task, since the compiler lets every
+// read of LDS wait for the K loads in flight, too.
+//
+// Decode steps are bound by reading: 64 tasks of 1k-16k keys (32 / 8 heads, d = 128, 4 bits) 69 us for
+// 0.33 GB of codes and sums, the rate of a large copy.  The votes of 32-64 tokens a task are bound
+// by issue, an exponential, a multiply-add and a sum per score beside the MFMAs: 16 tasks of 2k-16k
+// keys (28 / 4, bf16) 76 us, of 27 for the bytes or the FLOPs.  32 rows a trip took 1% more, blocks of
+// 32 keys 2% more, 6 waves a workgroup 45% more, rows staged two trips ahead 8% more.
 #include "attn_decode.h"
 #include "kv4.h"
 

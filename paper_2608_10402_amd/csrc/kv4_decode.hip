@@ -13,7 +13,16 @@
 // of one key at a time, and paired key by key with byte permutations.  Both products take bf16
 // operands, which hold code times scale exactly; sums, scores and softmax statistics are fp32,
 // and probabilities are rounded to bf16 for the second product as in the bf16 decode (its row sums
-// add the rounded ones, the log-sum-exp the exact ones).
+// add the rounded ones, the log-sum-exp the exact ones).  The MFMA that takes 4-bit operands was not
+// used for S^T: it adds products in groups with about 16 bits, 2^-14.7 of their sum of magnitudes
+// off, and the conversions are not what bounds the call.
+//
+// Bound by reading: 256 tasks of 1k-16k keys (32 / 8 heads, d = 128) take 384 us for 2.3 GB, 6.0
+// TB/s, against 367 us for the same loads with nothing done to them.  Two steps are in flight a
+// wave, at 2 waves a SIMD: three to five steps take the same time, 3 waves a SIMD 3-12% more, 4 spill.
+// A fifth fewer vector instructions changed nothing.  Short contexts add the merge of cut units to that:
+// 32 tasks with 2-8 tokens each 86 us, of which 19 after the last step (flags and partials through
+// memory; merged by whole workgroups 122 us).
 #include "attn_decode.h"
 #include "decode_runs.h"
 #include "kv4.h"

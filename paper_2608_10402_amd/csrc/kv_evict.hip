@@ -11,7 +11,7 @@
 // place a workgroup that loads a chunk of rows, waits for all of them (a barrier) and only then
 // stores them is right if it takes its chunks in order: later chunks read positions beyond every
 // slot written so far, which also lets it load the next chunk before it stores one.  Into new pages
-// the chunks are independent and go to workgroups of their own.
+// the chunks are independent and go to workgroups of their own.  The largest tasks come first.
 #include "kernels.h"
 #include "kv4.h"
 
@@ -183,17 +183,31 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMove = 1024;  // threads
-// Rows a thread has under way, in each of two chunks.  The move is bound by memory where the rows of a
-// workgroup's two chunks cover its latency: 64 tasks cut to half of 2k-16k positions in place (28 / 4
-// heads, d = 128, bf16), call us: 512 threads with 4 rows 298, 6 282, 8 274, 1024 with 4 246, which is
-// the rate of a large copy (4.8 TB/s); with the positions looked up behind the last chunk's rows 349.
-constexpr int kInFlight = 4;
+// Workgroups that share a (task, kv head)'s K or V rows, and the rows that a thread has under way in each
+// of two chunks.  In place chunks follow each other, so the longest tasks are the call's end and a lone
+// task is a chain of latencies: two workgroups take half of each row (one line of 128 bytes).  Into new
+// pages the chunks themselves are spread.  Call us on fresh sums, half of the positions kept (64 tasks of
+// 2k-16k, 28 / 4 heads, d = 128, bf16, in place | the same into new pages | one task of 30k in place | 64
+// tasks, 32 / 8 heads, 4 bits, in place with 260 for reading the rows back):
+//   whole rows, 4 under way         335 | 309 | 171 | 690
+//   half rows, 4                    297 | 348 | 112 | 681
+//   half rows, 2                    306 | 311 | 125 | 656
+//   whole rows, 2                         295
+// 512 threads are 4-15% slower than 1024 in place.  The first takes 42 us to select and 255 to move 1.2 GB,
+// the rate of a large copy (4.8 TB/s).  4-bit rows are pieces of 16 and 4 bytes all over their pages, so every
+// line of a page is read for the half of it that stays.
+template <int D, bool kKv4, bool kInPlace>
+constexpr int move_parts = kInPlace && (kKv4 || D == 128) ? 2 : 1;
+template <bool kKv4, bool kInPlace>
+constexpr int move_in_flight = kInPlace && !kKv4 ? 4 : 2;
 
-// The pieces of one token's K or V row: kLanes lanes of kBytes each.
+// The pieces of one token's K or V row: kLanes of kBytes each.
+// Pieces of kRun slots lie next to each other.
 template <int D, bool kKv4, bool kV>
 struct MoveRow {
   static constexpr int kLanes = kKv4 ? (kV ? 16 : 4) : D / 8;
   static constexpr int kBytes = kKv4 ? (kV ? D / 32 : D / 8) : 16;
+  static constexpr int kRun = kKv4 ? (kV ? 4 : 16) : 1;
 };
 
 template <int kBytes>
@@ -221,14 +235,17 @@ struct Piece {
   }
 };
 
-template <int D, bool kKv4, bool kV>
-__device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictTask& t, int head, int chunk_first,
+template <int D, bool kKv4, bool kV, bool kInPlace>
+__device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictTask& t, int head, int part, int chunk_first,
                                           int chunk_step) {
   using M = MoveRow<D, kKv4, kV>;
   using F = Kv4<D>;
-  constexpr int kRows = kMove / M::kLanes;  // rows a load
+  constexpr int kInFlight = move_in_flight<kKv4, kInPlace>;
+  constexpr int kLanes = M::kLanes / move_parts<D, kKv4, kInPlace>, kRun = M::kRun;
+  constexpr int kRows = kMove / kLanes;  // rows a load
   constexpr int kChunk = kRows * kInFlight;
-  const int lane = threadIdx.x % M::kLanes, r0 = threadIdx.x / M::kLanes;
+  const int lane = part * kLanes + threadIdx.x / kRun % kLanes;  // piece
+  const int r0 = threadIdx.x / (kRun * kLanes) * kRun + threadIdx.x % kRun;
   const int64_t out0 = (int64_t)t.first * a.num_kv_heads + (int64_t)head * t.keep;
   uint8_t* pool = kV && !kKv4 ? a.v_pool : a.k_pool;
   constexpr int64_t kBlk = kKv4 ? F::kBlock : (int64_t)kPage * D * 2;
@@ -316,16 +333,18 @@ __device__ __forceinline__ void move_mass(const EvictArgs& a, const EvictTask& t
   }
 }
 
-// grid: (task, kv head) x (K, V with the sums) x chunk groups
-template <int D, bool kKv4>
+// grid: (task, from the largest, kv head, part of the rows, K or V with the sums) x chunk groups
+template <int D, bool kKv4, bool kInPlace>
 __global__ __launch_bounds__(kMove) void evict_move_kernel(EvictArgs a) {
-  const int unit = blockIdx.x / a.num_kv_heads, head = blockIdx.x - unit * a.num_kv_heads;
-  const EvictTask t = a.move_tasks[unit];
-  if (blockIdx.y == 0) {
-    move_rows<D, kKv4, false>(a, t, head, blockIdx.z, gridDim.z);
+  constexpr int kParts = move_parts<D, kKv4, kInPlace>;
+  const int x = blockIdx.x / (2 * kParts), part = blockIdx.x / 2 % kParts;
+  const int nth = x / a.num_kv_heads, head = x - nth * a.num_kv_heads;
+  const EvictTask t = a.move_tasks[a.move_tasks[nth].nth];
+  if (blockIdx.x % 2 == 0) {
+    move_rows<D, kKv4, false, kInPlace>(a, t, head, part, blockIdx.y, gridDim.y);
   } else {
-    move_rows<D, kKv4, true>(a, t, head, blockIdx.z, gridDim.z);
-    move_mass(a, t, head, blockIdx.z * kMove + threadIdx.x, gridDim.z * kMove);
+    move_rows<D, kKv4, true, kInPlace>(a, t, head, part, blockIdx.y, gridDim.y);
+    if (part == 0) move_mass(a, t, head, blockIdx.y * kMove + threadIdx.x, gridDim.y * kMove);
   }
 }
 
@@ -335,17 +354,24 @@ hipError_t launch(const EvictArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(evict_select_kernel, dim3(units), dim3(kSelect), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // in place one workgroup takes its rows' chunks in order
-  const unsigned chunks = a.new_table == a.block_table ? 1u : (unsigned)min(64, (a.longest_keep + 255) / 256);
-  hipLaunchKernelGGL((evict_move_kernel<D, kKv4>), dim3(units, 2, chunks), dim3(kMove), 0, stream, a);
+  if (a.new_table == a.block_table)
+    hipLaunchKernelGGL((evict_move_kernel<D, kKv4, true>), dim3(units * 2 * move_parts<D, kKv4, true>), dim3(kMove), 0,
+                       stream, a);
+  else
+    hipLaunchKernelGGL((evict_move_kernel<D, kKv4, false>),
+                       dim3(units * 2, (unsigned)min(64, (a.longest_keep + 255) / 256)), dim3(kMove), 0, stream, a);
   return hipGetLastError();
 }
 
 // Every variant is instantiated explicitly (see attn_decode.hip).
-template __global__ void evict_move_kernel<128, false>(EvictArgs);
-template __global__ void evict_move_kernel<128, true>(EvictArgs);
-template __global__ void evict_move_kernel<64, false>(EvictArgs);
-template __global__ void evict_move_kernel<64, true>(EvictArgs);
+template __global__ void evict_move_kernel<128, false, false>(EvictArgs);
+template __global__ void evict_move_kernel<128, false, true>(EvictArgs);
+template __global__ void evict_move_kernel<128, true, false>(EvictArgs);
+template __global__ void evict_move_kernel<128, true, true>(EvictArgs);
+template __global__ void evict_move_kernel<64, false, false>(EvictArgs);
+template __global__ void evict_move_kernel<64, false, true>(EvictArgs);
+template __global__ void evict_move_kernel<64, true, false>(EvictArgs);
+template __global__ void evict_move_kernel<64, true, true>(EvictArgs);
 
 }  // namespace kern
 

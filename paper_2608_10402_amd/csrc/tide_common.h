@@ -468,7 +468,8 @@ struct EvictTask {
   int32_t keep;
   int32_t recent;
   int32_t first;   // packed row of `kept`: the sum of the earlier tasks' keep
-  int32_t pad[3];
+  int32_t nth;     // of record i: the record of the task with the i-th largest `keep`
+  int32_t pad[2];
 };
 
 // A kept position: its sum, and the pages that it leaves and that its rank lies in (leaves < 0: one of
