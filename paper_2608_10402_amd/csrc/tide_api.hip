@@ -137,6 +137,14 @@ int wait_slot(StagingSlot& s) {
   return TIDE_OK;
 }
 
+// A slot whose reader's launch reported an error, which does not say that it is not queued: of a call's
+// two launches the second may have failed, or the error may be one that an earlier call of the program
+// left behind.  Once the stream is idle nothing reads the slot, and nobody waits for its flags.
+void release_unread(StagingSlot& s, hipStream_t stream) {
+  (void)hipStreamSynchronize(stream);
+  s.pending = false;
+}
+
 struct DeviceStaging {
   StagingSlot slots[kStagingSlots];
   int next = 0;
@@ -246,7 +254,10 @@ int upload(const Plan& plan, void* workspace, hipStream_t stream, uint32_t reade
   hipLaunchKernelGGL(stage_copy_kernel, dim3(nblocks), dim3(256), 0, stream,
                      static_cast<u32x4_t*>(workspace), static_cast<const u32x4_t*>(s.dev), n16,
                      s.flags_dev, s.seq);
-  if (hipGetLastError() != hipSuccess) return TIDE_ERR_HIP;
+  if (hipGetLastError() != hipSuccess) {
+    release_unread(s, stream);
+    return TIDE_ERR_HIP;
+  }
   s.nblocks = nblocks;
   s.pending = true;
   out->plan = static_cast<const uint8_t*>(workspace);
@@ -254,7 +265,7 @@ int upload(const Plan& plan, void* workspace, hipStream_t stream, uint32_t reade
 }
 
 int finish(hipError_t launch_status, Staged& st, void* workspace, hipStream_t stream) {
-  if (st.slot && launch_status != hipSuccess) st.slot->pending = false;  // nothing will read it
+  if (st.slot && launch_status != hipSuccess) release_unread(*st.slot, stream);
   if (st.lock.owns_lock()) st.lock.unlock();
   if (launch_status != hipSuccess) return TIDE_ERR_HIP;
   if (!debug_checks()) return TIDE_OK;
