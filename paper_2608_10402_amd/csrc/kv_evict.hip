@@ -60,13 +60,13 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
   __shared__ uint32_t tmp[2][kSelect / 64];
   __shared__ uint32_t found[3];  // digit, keys above it, keys with it
   const int tid = threadIdx.x;
-  const int unit = blockIdx.x / a.num_kv_heads, head = blockIdx.x - unit * a.num_kv_heads;
+  const int pair = a.first_pair + blockIdx.x, unit = pair / a.num_kv_heads, head = pair - unit * a.num_kv_heads;
   __shared__ EvictTask task;
   if (tid == 0) task = a.tasks[unit];
   __syncthreads();
   const EvictTask t = task;
   if (tid == 0) {
-    if (a.reads.done) plan_read(a.reads, blockIdx.x);
+    if (a.reads.done) plan_read(a.reads, pair);
     if (head == 0) a.move_tasks[unit] = t;  // for the move, which comes after the slot's release
   }
   const int32_t* row = a.block_table + (int64_t)t.task * a.bt_stride;
@@ -337,7 +337,7 @@ __device__ __forceinline__ void move_mass(const EvictArgs& a, const EvictTask& t
 template <int D, bool kKv4, bool kInPlace>
 __global__ __launch_bounds__(kMove) void evict_move_kernel(EvictArgs a) {
   constexpr int kParts = move_parts<D, kKv4, kInPlace>;
-  const int x = blockIdx.x / (2 * kParts), part = blockIdx.x / 2 % kParts;
+  const int x = a.first_pair + blockIdx.x / (2 * kParts), part = blockIdx.x / 2 % kParts;
   const int nth = x / a.num_kv_heads, head = x - nth * a.num_kv_heads;
   const EvictTask t = a.move_tasks[a.move_tasks[nth].nth];
   if (blockIdx.x % 2 == 0) {
@@ -348,19 +348,33 @@ __global__ __launch_bounds__(kMove) void evict_move_kernel(EvictArgs a) {
   }
 }
 
+// Both kernels over all pairs, as many a launch as leave it less than 2^32 threads.
 template <int D, bool kKv4>
-hipError_t launch(const EvictArgs& a, hipStream_t stream) {
-  const unsigned units = (unsigned)a.num_tasks * a.num_kv_heads;
-  hipLaunchKernelGGL(evict_select_kernel, dim3(units), dim3(kSelect), 0, stream, a);
-  hipError_t e = hipGetLastError();
+hipError_t launch(EvictArgs a, hipStream_t stream) {
+  const bool in_place = a.new_table == a.block_table;
+  const int64_t pairs = (int64_t)a.num_tasks * a.num_kv_heads;
+  auto in_turn = [&](int groups, int threads, auto&& kernel) {  // groups: workgroups of a pair
+    const int64_t most = (((int64_t)1 << 32) - 1) / (groups * threads);
+    for (int64_t at = 0; at < pairs; at += most) {
+      a.first_pair = (int32_t)at;
+      kernel((unsigned)(min(most, pairs - at) * groups));
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  };
+  const hipError_t e = in_turn(1, kSelect, [&](unsigned n) {
+    hipLaunchKernelGGL(evict_select_kernel, dim3(n), dim3(kSelect), 0, stream, a);
+  });
   if (e != hipSuccess) return e;
-  if (a.new_table == a.block_table)
-    hipLaunchKernelGGL((evict_move_kernel<D, kKv4, true>), dim3(units * 2 * move_parts<D, kKv4, true>), dim3(kMove), 0,
-                       stream, a);
-  else
-    hipLaunchKernelGGL((evict_move_kernel<D, kKv4, false>),
-                       dim3(units * 2, (unsigned)min(64, (a.longest_keep + 255) / 256)), dim3(kMove), 0, stream, a);
-  return hipGetLastError();
+  if (in_place)
+    return in_turn(2 * move_parts<D, kKv4, true>, kMove, [&](unsigned n) {
+      hipLaunchKernelGGL((evict_move_kernel<D, kKv4, true>), dim3(n), dim3(kMove), 0, stream, a);
+    });
+  return in_turn(2, kMove, [&](unsigned n) {
+    hipLaunchKernelGGL((evict_move_kernel<D, kKv4, false>), dim3(n, (unsigned)min(64, (a.longest_keep + 255) / 256)),
+                       dim3(kMove), 0, stream, a);
+  });
 }
 
 // Every variant is instantiated explicitly (see attn_decode.hip).

@@ -492,6 +492,7 @@ struct EvictArgs {
   int32_t new_stride;
   int32_t num_kv_heads;
   int32_t num_tasks;
+  int32_t first_pair;  // of the launch's (task, kv head) pairs
   int32_t longest_keep;
   const EvictTask* tasks;
   EvictTask* move_tasks;  // the same in the workspace, written by the first kernel for the second
