@@ -211,7 +211,7 @@ struct MoveRow {
 };
 
 template <int kBytes>
-struct Piece {
+struct MovePiece {
   uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
   __device__ __forceinline__ void load(const uint8_t* p) {
     if constexpr (kBytes == 16) {
@@ -263,7 +263,7 @@ __device__ __forceinline__ void move_rows(const EvictArgs& a, const EvictTask& t
     else return blk + F::k_scale(16 * lane + slot);
   };
   struct Chunk {
-    Piece<M::kBytes> x[kInFlight];
+    MovePiece<M::kBytes> x[kInFlight];
     uint32_t scale[kInFlight];
     int32_t to[kInFlight];  // page, or -1: not moved
   };
