@@ -414,8 +414,10 @@ TIDE_API int tide_kv4_extend_attn(const void* q, const void* kv4_pool, int64_t n
  *   counted_lens  positions whose sums are carried on (at most prefix + extend); NULL: prefix_lens,
  *                 so that the new tokens' own sums start at 0
  * Tokens of which only the last w are to count: prefix + extend - w and w, with counted_lens = the
- * prefix.  fp32 throughout, one writer per sum; two tasks must not map the same page (a sum of
- * theirs is unspecified).  Workspace: TIDE_OP_ATTN_MASS.
+ * prefix.  fp32 throughout, one writer per sum; two tasks of a call must not map the same page (a sum
+ * of theirs is unspecified).  Tasks that share pages (a GRPO group's prompt) go into calls of their own,
+ * one after the other: each adds its rows' weights to the shared keys' sums.  Workspace:
+ * TIDE_OP_ATTN_MASS.
  */
 TIDE_API int tide_attn_mass(const void* q, const float* lse, const void* k_pool, int64_t num_pages,
                    const int32_t* block_table, int32_t bt_stride, int32_t num_tasks,

@@ -171,7 +171,8 @@ class PagedKV(_Paged):
         return out
 
     def attn_mass(self, q, lse, prefix_lens, extend_lens, mass, counted_lens=None, stream=None):
-        """Add the attention weights of the new tokens' rows to the keys' sums (tide_attn_mass)."""
+        """Add the attention weights of the new tokens' rows to the keys' sums (tide_attn_mass).
+        Tasks that share pages go into calls of their own."""
         self._call(lambda: _lib.tide_workspace_size(_lib.TIDE_OP_ATTN_MASS, prefix_lens, extend_lens,
                                                     self.dims),
                    lambda ws: _lib.tide_attn_mass(q, lse, self.k_pool, self.block_table, prefix_lens,
@@ -252,7 +253,8 @@ class PagedKV4(_Paged):
         return out
 
     def attn_mass(self, q, lse, prefix_lens, extend_lens, mass, counted_lens=None, stream=None):
-        """Add the attention weights of the new tokens' rows to the keys' sums (tide_attn_mass)."""
+        """Add the attention weights of the new tokens' rows to the keys' sums (tide_attn_mass).
+        Tasks that share pages go into calls of their own."""
         self._call(self._size(_lib.TIDE_OP_ATTN_MASS, prefix_lens, extend_lens),
                    lambda ws: _lib.tide_kv4_attn_mass(q, lse, self.pool, self.block_table, prefix_lens,
                                                       extend_lens, self.dims, mass, counted_lens, ws,
