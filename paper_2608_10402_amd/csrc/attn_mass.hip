@@ -9,8 +9,9 @@
 // the end, in a fixed order.  Every sum has one writer: no atomics, and repeated calls give the
 // same bits.  Scores, weights and sums are fp32.
 //
-// The blocks of all tasks, laid end to end, are cut into runs of equal cost (rows and reads), and
-// one wave takes a run of one kv head, the next block's loads behind the last rows of one.
+// The blocks of all tasks, laid end to end, are cut into runs of near equal cost (rows and reads; whole
+// blocks, so that runs of few differ much), and one wave takes a run of one kv head, the next block's
+// loads behind the last rows of one.
 // Query rows pass through a wave's own 4 KB of LDS, whole rows at a time, the next 16 on their way
 // while 16 are used: as operands straight from memory, 64 lanes read 64 separate pieces, which
 // kept the L1 busy for 73% of a call of 43 rows x 7 heads.  Where 16 rows are all of every task's
@@ -18,9 +19,13 @@
 // read of LDS wait for the K loads in flight, too.
 //
 // Decode steps are bound by reading: 64 tasks of 1k-16k keys (32 / 8 heads, d = 128, 4 bits) 69 us for
-// 0.33 GB of codes and sums, the rate of a large copy.  The votes of 32-64 tokens a task are bound
-// by issue, an exponential, a multiply-add and a sum per score beside the MFMAs: 16 tasks of 2k-16k
-// keys (28 / 4, bf16) 76 us, of 27 for the bytes or the FLOPs.  32 rows a trip took 1% more, blocks of
+// 0.33 GB of codes and sums, the rate of a large copy; over bf16 keys 233 us for 1.13 GB.
+// The votes of 32-64 tokens a task are far from it: 16 tasks of 2k-16k keys (28 / 4) 76 us over bf16
+// and 70 over 4 bits, of 27 for the bytes or the FLOPs.  A trip issues 88 vector instructions beside
+// its MFMAs, of which the scores' exponential, multiply-add and sum are 48, and 88 scalar ones: the
+// others find the next rows (descriptors, divisions by the group).  Runs there are 2 or 3 blocks (the
+// mean costs 0.68 of the longest), so 1.8 of 3 waves a SIMD live over the kernel, vector instructions
+// issue in 35% of the SIMDs' cycles and MFMAs run in 18%.  32 rows a trip took 1% more, blocks of
 // 32 keys 2% more, 6 waves a workgroup 45% more, rows staged two trips ahead 8% more.
 #include "attn_decode.h"
 #include "kv4.h"

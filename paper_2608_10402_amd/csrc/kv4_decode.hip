@@ -1,8 +1,8 @@
-// Attention of a few query tokens a task over the 4-bit cache: decode, and the extends of up to
-// kKv4DirectTokens tokens (plan.h).
+// Attention of a few query tokens a task over the 4-bit cache: decode, and the extends that read the
+// codes themselves (kKv4DirectUnits in plan.cpp).
 //
-// A unit is 1 .. 16 / G consecutive query tokens of a task; their (token, query head) rows of one kv
-// head are the columns of 16x16x32 MFMAs, a step is 32 keys (2 pages).  As in
+// A unit is 1 .. 32 / G consecutive query tokens of a task (one, of decode); their (token, query head)
+// rows of one kv head are the columns of one or two 16x16x32 MFMAs, a step is 32 keys (2 pages).  As in
 // attn_decode_stream.hip the units' steps are laid end to end and cut into equal runs, one wave
 // takes a run of one kv head, and cut units are put together at the end (decode_runs.h).
 //
@@ -22,7 +22,9 @@
 // wave, at 2 waves a SIMD: three to five steps take the same time, 3 waves a SIMD 3-12% more, 4 spill.
 // A fifth fewer vector instructions changed nothing.  Short contexts add the merge of cut units to that:
 // 32 tasks with 2-8 tokens each 86 us, of which 19 after the last step (flags and partials through
-// memory; merged by whole workgroups 122 us).
+// memory; merged by whole workgroups 122 us).  Its other 67 us, of 41 to read the codes, have no one
+// bound: over the whole kernel 1.3 of 2 waves a SIMD live, a third of their time waits for memory,
+// vector instructions issue in 36% of the SIMDs' cycles and MFMAs run in 15%.
 #include "attn_decode.h"
 #include "decode_runs.h"
 #include "kv4.h"

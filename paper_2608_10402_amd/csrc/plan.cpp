@@ -1013,7 +1013,10 @@ constexpr int64_t kKv4StageItems = 1024;  // items that a short call is cut into
 // them.  Where the units that a key is read for are fewer than this, on average, the first is faster.
 // Call us, codes and unpacked, 32 tasks of 2k-16k keys: 28 / 4 heads, d = 128, 8 tokens (2 units) 73 and
 // 290, 24 (6) 179 and 310, 48 (12) 326 and 377, 64 (16) 426 and 394; 32 / 8 heads, 64 tokens (8) 463 and
-// 636; 32 / 2, d = 64, 8 tokens (4) 58 and 75, 16 (8) 97 and 90, 32 (16) 174 and 128.
+// 636; 32 / 2, d = 64, 8 tokens (4) 58 and 75, 16 (8) 97 and 90, 32 (16) 174 and 128.  The choice is the
+// whole call's, so one long extend has every task's pages unpacked: 32 tasks of 16k keys with one token
+// and one with 2,048 (28 / 4 heads) take 910 us and 1.04 GB, the two kinds in calls of their own 62 and
+// 411 us, 2 and 34 MB.
 constexpr int64_t kKv4DirectUnits = 12, kKv4DirectUnits64 = 7;
 
 // Appends `n` records to a plan's blob region at `off` (grown to its end) and returns the end.
