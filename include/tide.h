@@ -385,9 +385,10 @@ TIDE_API int tide_kv4_decode_append_attn(const void* q, const void* k_new, const
 /*
  * tide_extend_attn over a 4-bit pool (the new tokens appended before).  A call of a few tokens a task
  * reads the codes themselves; a larger one unpacks its tasks' pages into the workspace and attends
- * over those.  Workspace: TIDE_OP_KV4_EXTEND, up to 1 GiB of unpacked pages (one task's
- * if that is more).  A new token's V that is NaN or infinite may reach every row of its task in the call,
- * those before it too.
+ * over those.  It is one choice for the call, by the new tokens of all tasks, so a long extend among
+ * short ones is better off in a call of its own.  Workspace: TIDE_OP_KV4_EXTEND, up to 1 GiB of
+ * unpacked pages (one task's if that is more).  A new token's V that is NaN or infinite may reach every
+ * row of its task in the call, those before it too.
  */
 TIDE_API int tide_kv4_extend_attn(const void* q, const void* kv4_pool, int64_t num_pages,
                          const int32_t* block_table, int32_t bt_stride, int32_t num_tasks,

@@ -246,6 +246,8 @@ class PagedKV4(_Paged):
         return out
 
     def extend(self, q, prefix_lens, extend_lens, out=None, lse=None, stream=None):
+        """A long extend unpacks the pages of every task of its call into the workspace, which stays
+        with the pool object: one among short ones is better off in a call of its own."""
         out = torch.empty_like(q) if out is None else out
         self._call(self._size(_lib.TIDE_OP_KV4_EXTEND, prefix_lens, extend_lens),
                    lambda ws: _lib.tide_kv4_extend_attn(q, self.pool, self.block_table, prefix_lens,
