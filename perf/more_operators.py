@@ -8,12 +8,12 @@ positions.
   map      from every task's cached and wanted lengths: pages taken from the free list or given
            back, the block table's new entries, and the rows of the tokens that come in
   append   the rows' K/V into their slots, and the key bounds of the pages that changed
-  bounds   the key bounds of whole contexts: per page and kv head the least s in [-120, 121] with
+  bounds   the key bounds of whole contexts: per page and kv head the least s in [-120, 122] with
            max|k| <= 127 * 2^s, hi = ceil(max over the page's positions of k / 2^s) and
            lo = floor(min of k / 2^s), entry by entry; s = 127, hi = lo = 0 where a key is not finite
   select   per row and kv head, the blocks to attend to: the first `sink`, the last `recent`, and
            the others with the highest score, `budget` in all, ascending, -1 behind them.  With
-           t the least in [-120, 121] such that max|q| <= 127 * 2^t and c = q / 2^t to the nearest
+           t the least in [-120, 122] such that max|q| <= 127 * 2^t and c = q / 2^t to the nearest
            whole number (ties to even), the score of a block is the largest over the kv head's query
            heads of 2^clamp(s + t, -100, 100) * sum over entries of max(c * hi, c * lo): whole
            numbers times a power of two, so every score is exact and the choice has one answer
@@ -195,10 +195,10 @@ def _key_bounds(k):
 
 
 def _unit(top):
-    """The least s in [-120, 121] with top <= 127 * 2^s."""
+    """The least s in [-120, 122] with top <= 127 * 2^s."""
     mant, ex = torch.frexp(top)  # top = mant 2^ex, mant in [1/2, 1)
     s = ex - 7 + (mant > 127.0 / 128.0)
-    return torch.where(top > 0, s, -120).clamp(-120, 121)
+    return torch.where(top > 0, s, -120).clamp(-120, 122)
 
 
 def _choose(score, blocks, budget, sink, recent):
@@ -519,9 +519,9 @@ def _exact_map(s):
 
 
 def _exact_unit(top):
-    """The least s in [-120, 121] with top <= 127 * 2^s, by trying them."""
-    s = torch.full(top.shape, 121, dtype=torch.int64, device=top.device)
-    for e in range(120, -121, -1):
+    """The least s in [-120, 122] with top <= 127 * 2^s, by trying them."""
+    s = torch.full(top.shape, 122, dtype=torch.int64, device=top.device)
+    for e in range(121, -121, -1):
         s = torch.where(top <= 127.0 * 2.0 ** e, e, s)
     return s
 
