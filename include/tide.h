@@ -120,7 +120,11 @@ enum {
   TIDE_OP_KV4_DECODE = 7, /* tide_kv4_decode_attn, tide_kv4_decode_append_attn */
   TIDE_OP_KV4_EXTEND = 8,
   TIDE_OP_ATTN_MASS = 9, /* tide_attn_mass, tide_kv4_attn_mass */
-  TIDE_OP_KV_EVICT = 10  /* tide_kv_evict, tide_kv4_evict */
+  TIDE_OP_KV_EVICT = 10, /* tide_kv_evict, tide_kv4_evict */
+  TIDE_OP_SLOT_APPEND = 11,  /* of tide_rows_workspace_size, as the following */
+  TIDE_OP_KEY_BOUNDS = 12,
+  TIDE_OP_BLOCK_SELECT = 13,
+  TIDE_OP_SPARSE_ATTN = 14
 };
 
 /* Attention shape shared by all calls. */
@@ -465,6 +469,108 @@ TIDE_API int tide_kv4_evict(void* kv4_pool, float* mass_pool, int64_t num_pages,
                    int32_t new_bt_stride, int32_t num_tasks, const int32_t* kv_lens,
                    const int32_t* keep_lens, const int32_t* recent_lens, const tide_dims* dims,
                    int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- steps whose lengths live on the device, and attention over a budget of blocks ----------------
+ *
+ * The calls above take lengths from the host and read whole contexts.  These take both from the
+ * device: a captured graph of them goes on as the tasks' contexts grow, and a step over a long
+ * context reads the blocks that matter to it.  bf16 pools; shapes, streams and errors as above;
+ * device buffers of K, V, Q, outputs, bounds and workspace 16-byte aligned (TIDE_ERR_INVALID_ARG).
+ *
+ *   row          one query token: row_task[r] and row_pos[r] (device int32) are its block-table row and
+ *                its position, row_slot[r] (device int64) the pool slot page * 16 + slot of its K/V.  A row
+ *                whose task or position is negative or out of range is padding: nothing is read or written
+ *                for it, its outputs stay as they are.
+ *   block        the 16 positions of a page; logical block i of a task holds positions 16 i .. 16 i + 15
+ *   key bounds   int8 bounds[num_pages][num_kv_heads][2][head_dim] and units[num_pages][num_kv_heads]: with s the
+ *                least integer in [-120, 122] such that max|k| <= 127 * 2^s over a page's positions and
+ *                entries, bounds[.][.][0] = ceil(max of k / 2^s) and [1] = floor(min of k / 2^s), entry by
+ *                entry, units = s; a page with a key that is not finite has unit 127 and zeros
+ *
+ * Workspace: tide_rows_workspace_size; num_rows, budget and max_len as the call gets them (budget: attention;
+ * max_len: selection, the longest context, > 0).  It holds nothing between calls.
+ */
+TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, int32_t max_len,
+                             const tide_dims* dims, size_t* bytes_out);
+
+/*
+ * Block tables and slot maps from lengths on the device.  All arrays are device memory.
+ *   lens, want_lens  int32 [num_tasks]: positions that are cached and that are wanted
+ *   free_pages       int32 [free_capacity], of which the first *free_count are free: a stack
+ *   lens_out         int32 [num_tasks], may be lens itself; free_count_out may be free_count
+ *   row_start        int32 [num_tasks + 1]: the first row of each task
+ *   row_*            [num_rows]: the new tokens' rows, in task order; padding (-1) behind them
+ * First every task with want < lens gives its pages from ceil(want / 16) on back, in task order and from
+ * the first of them on (what does not fit in free_capacity is dropped).  Then, in task order, a task
+ * with want > lens gets want - lens rows and ceil(want / 16) - ceil(lens / 16) pages from the top of the
+ * stack.  A task is refused if its rows would end past num_rows, or if it needs a page and the pages that it
+ * and the tasks before it need (refused ones too, for want of pages) are more than there are: then
+ * lens_out == lens != want, its block-table row stays as it is, and its rows, if num_rows has room for them,
+ * are padding.  A task whose lens or want is negative or above 16 * bt_stride is left alone, without rows.
+ * Entries of free_pages and of block_table that no page is put into keep what they hold.  A page that two
+ * tasks share must not be given back by both.  num_tasks * bt_stride < 2^31 and num_rows < 2^31 - 1
+ * (TIDE_ERR_UNSUPPORTED).  num_tasks == 0: nothing is written.
+ */
+TIDE_API int tide_page_map(const int32_t* lens, const int32_t* want_lens, int32_t num_tasks, int32_t* block_table,
+                  int32_t bt_stride, int32_t* free_pages, int32_t free_capacity, const int32_t* free_count,
+                  int32_t num_rows, int32_t* lens_out, int32_t* free_count_out, int32_t* row_start,
+                  int32_t* row_task, int32_t* row_pos, int64_t* row_slot, const tide_dims* dims, void* stream);
+
+/*
+ * tide_kv_append by slots: the K/V of row r (k_new / v_new: bf16 [num_rows][Hkv][d]) go to slot row_slot[r],
+ * bit-exact; a negative slot is padding, one past the pool is skipped and flagged like a page id out of
+ * range.  With bounds and units (both or neither NULL) the key bounds of the pages that changed are
+ * brought up to date; that takes the page's slots before the new ones to hold keys of the same
+ * task, and a page's new rows to follow each other in slot order (the rows of tide_page_map do;
+ * otherwise the page's bounds are unspecified).  Two rows of one slot: either's.
+ */
+TIDE_API int tide_slot_append(const void* k_new, const void* v_new, const int64_t* row_slot, int32_t num_rows,
+                     void* k_pool, void* v_pool, int64_t num_pages, int8_t* bounds, int8_t* units,
+                     const tide_dims* dims, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Key bounds of the pages that hold positions from_lens[b] .. lens[b] - 1 of each task (device int32; from_lens
+ * NULL: 0), from all of a page's positions below lens[b]: for contexts that other calls wrote or moved.
+ * Bounds of other pages stay as they are, and of a page id out of range none are written.  max_len: no
+ * position at or past it is looked at (0: 16 * bt_stride, and at most that, else TIDE_ERR_CAPACITY); the call's
+ * time grows with it.  Tasks that share a page and fill it differently: either's bounds.
+ */
+TIDE_API int tide_key_bounds(const void* k_pool, int64_t num_pages, const int32_t* block_table, int32_t bt_stride,
+                    int32_t num_tasks, const int32_t* lens, const int32_t* from_lens, int32_t max_len,
+                    int8_t* bounds, int8_t* units, const tide_dims* dims, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/*
+ * The blocks that each row attends to, per KV head: of the row_pos / 16 + 1 blocks up to its position the
+ * first `sink`, the last `recent` and, of the others, those with the highest score, `budget` in all (sink +
+ * recent <= budget); all of them where they are no more than that.
+ *   sel   int32 [num_rows][Hkv][budget] (device): ascending, -1 behind them
+ * Score.  With t_h the least integer in [-120, 122] such that max|q_h| <= 127 * 2^t_h and c_h = q_h / 2^t_h to
+ * the nearest integer (ties to even):
+ *     score = max over the KV head's query heads h of
+ *             2^min(100, max(-100, unit + t_h)) * sum_i max(c_hi * upper_i, c_hi * lower_i)
+ * which is exact (no key's product with the whole-number query exceeds it); equal scores: the earlier block.
+ * A block of unit 127 scores +inf, one whose page id is out of range -inf; a query head with a NaN or an
+ * infinity counts as zeros.  max_len: rows at positions at or past it are padding (0: 16 * bt_stride, and at
+ * most that, else TIDE_ERR_CAPACITY); workspace and time grow with it.
+ */
+TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int32_t* row_pos, int32_t num_rows,
+                      const int8_t* bounds, const int8_t* units, int64_t num_pages,
+                      const int32_t* block_table, int32_t bt_stride, int32_t num_tasks, int32_t budget,
+                      int32_t sink, int32_t recent, int32_t max_len, const tide_dims* dims, int32_t* sel,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of each row over the positions at or before its own in the blocks that sel[row][KV head] lists,
+ * in any order; an entry that is negative, past the row's position or whose page id is out of range
+ * adds nothing, and a block listed twice counts twice.  q/out: bf16 [num_rows][Hq][d]; lse: fp32
+ * [num_rows][Hq] or NULL.  A row of which no entry adds anything gets zeros, and an lse of -inf.
+ */
+TIDE_API int tide_sparse_attn(const void* q, const void* k_pool, const void* v_pool, int64_t num_pages,
+                     const int32_t* block_table, int32_t bt_stride, int32_t num_tasks,
+                     const int32_t* row_task, const int32_t* row_pos, int32_t num_rows, const int32_t* sel,
+                     int32_t budget, const tide_dims* dims, void* out, float* lse, void* workspace,
+                     size_t workspace_bytes, void* stream);
 
 /* Human-readable text for a status code (static storage, never NULL). */
 TIDE_API const char* tide_status_string(int status);

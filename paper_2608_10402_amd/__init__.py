@@ -3,7 +3,8 @@ Continuous Task Batching (arXiv 2608.10402) -- KV-append, extend attention over 
 retained paged prefix, split-K decode attention (also over prompt prefixes shared by a
 GRPO group, and with the decoded token's append fused in), full re-prefill for
 comparison, a cache held in 4 bits with the attention that reads it, eviction by accumulated
-attention weight, and the task-batching scheduler that drives them (ctb).
+attention weight, steps whose lengths live on the device with attention over a budget of blocks,
+and the task-batching scheduler that drives them (ctb).
 
 The compute lives in libtide.so (hand-written HIP kernels behind the C ABI of
 include/tide.h).  This package is its ctypes binding plus a small pool helper.
@@ -20,8 +21,10 @@ from ._lib import (TIDE_ERR_CAPACITY, TIDE_ERR_HIP, TIDE_ERR_INVALID_ARG, TIDE_E
                    TIDE_OP_KV4_UNPACK, TIDE_OP_KV_EVICT, kv4_block_bytes, tide_attn_mass,
                    tide_kv4_append, tide_kv4_attn_mass, tide_kv4_decode_append_attn,
                    tide_kv4_decode_attn, tide_kv4_evict, tide_kv4_extend_attn, tide_kv4_unpack,
-                   tide_kv_evict)
-from .kvcache import PagedKV, PagedKV4
+                   tide_kv_evict, TIDE_OP_BLOCK_SELECT, TIDE_OP_KEY_BOUNDS, TIDE_OP_SLOT_APPEND,
+                   TIDE_OP_SPARSE_ATTN, tide_block_select, tide_key_bounds, tide_page_map,
+                   tide_rows_workspace_size, tide_slot_append, tide_sparse_attn)
+from .kvcache import PagedKV, PagedKV4, PageTable
 
 __all__ = ["TIDE_ERR_CAPACITY", "TIDE_ERR_HIP", "TIDE_ERR_INVALID_ARG", "TIDE_ERR_PAGE_RANGE",
            "TIDE_ERR_UNSUPPORTED", "TIDE_OK", "TIDE_OP_DECODE", "TIDE_OP_EXTEND",
@@ -34,4 +37,7 @@ __all__ = ["TIDE_ERR_CAPACITY", "TIDE_ERR_HIP", "TIDE_ERR_INVALID_ARG", "TIDE_ER
            "TIDE_OP_KV4_DECODE", "TIDE_OP_KV4_EXTEND", "TIDE_OP_KV4_UNPACK", "TIDE_OP_KV_EVICT",
            "kv4_block_bytes", "tide_attn_mass", "tide_kv4_append", "tide_kv4_attn_mass",
            "tide_kv4_decode_append_attn", "tide_kv4_decode_attn", "tide_kv4_evict",
-           "tide_kv4_extend_attn", "tide_kv4_unpack", "tide_kv_evict"]
+           "tide_kv4_extend_attn", "tide_kv4_unpack", "tide_kv_evict", "PageTable",
+           "TIDE_OP_BLOCK_SELECT", "TIDE_OP_KEY_BOUNDS", "TIDE_OP_SLOT_APPEND", "TIDE_OP_SPARSE_ATTN",
+           "tide_block_select", "tide_key_bounds", "tide_page_map", "tide_rows_workspace_size",
+           "tide_slot_append", "tide_sparse_attn"]

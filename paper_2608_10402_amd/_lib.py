@@ -32,6 +32,10 @@ TIDE_OP_KV4_DECODE = 7
 TIDE_OP_KV4_EXTEND = 8
 TIDE_OP_ATTN_MASS = 9
 TIDE_OP_KV_EVICT = 10
+TIDE_OP_SLOT_APPEND = 11
+TIDE_OP_KEY_BOUNDS = 12
+TIDE_OP_BLOCK_SELECT = 13
+TIDE_OP_SPARSE_ATTN = 14
 
 # bytes of the static device scratch of tide_decode_attn_noalloc (TIDE_NOALLOC_SCRATCH_BYTES)
 NOALLOC_SCRATCH_BYTES = 64 << 20
@@ -42,6 +46,8 @@ EXPORTED = ("tide_workspace_size", "tide_kv_append", "tide_extend_attn", "tide_d
             "tide_kv4_append", "tide_kv4_unpack", "tide_kv4_decode_attn",
             "tide_kv4_decode_append_attn", "tide_kv4_extend_attn", "tide_attn_mass",
             "tide_kv4_attn_mass", "tide_kv_evict", "tide_kv4_evict",
+            "tide_rows_workspace_size", "tide_page_map", "tide_slot_append", "tide_key_bounds",
+            "tide_block_select", "tide_sparse_attn",
             "tide_plan_info_get", "tide_ctb_create", "tide_ctb_step", "tide_ctb_get_stats", "tide_ctb_destroy",
             "tide_status_string", "tide_shutdown")
 
@@ -116,6 +122,15 @@ def load(path: str = LIB_PATH):
                                   sz, vp]
     lib.tide_kv4_evict.argtypes = [vp, vp, i64, vp, i32, vp, i32, i32, vp, vp, vp, dims_p, vp, vp,
                                    sz, vp]
+    lib.tide_rows_workspace_size.argtypes = [ctypes.c_int, i32, i32, i32, dims_p, ctypes.POINTER(sz)]
+    lib.tide_page_map.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, dims_p,
+                                  vp]
+    lib.tide_slot_append.argtypes = [vp, vp, vp, i32, vp, vp, i64, vp, vp, dims_p, vp, sz, vp]
+    lib.tide_key_bounds.argtypes = [vp, i64, vp, i32, i32, vp, vp, i32, vp, vp, dims_p, vp, sz, vp]
+    lib.tide_block_select.argtypes = [vp, vp, vp, i32, vp, vp, i64, vp, i32, i32, i32, i32, i32, i32, dims_p,
+                                      vp, vp, sz, vp]
+    lib.tide_sparse_attn.argtypes = [vp, vp, vp, i64, vp, i32, i32, vp, vp, i32, vp, i32, dims_p, vp, vp, vp,
+                                     sz, vp]
     lib.tide_plan_info_get.argtypes = [ctypes.c_int, i32, vp, vp, dims_p, i32,
                                        ctypes.POINTER(tide_plan_info)]
     lib.tide_ctb_create.argtypes = [vp, i32, vp, vp, i32, vp, vp, vp, vp, vp,
@@ -695,6 +710,136 @@ def tide_kv4_evict(kv4_pool, mass, block_table, kv_lens, keep_lens, dims: tide_d
             _dev(block_table, torch.int32, "block_table"), int(block_table.shape[1]), new_p, stride,
             int(hold[0].size), n_p, k_p, r_p, ctypes.byref(dims),
             _dev(kept, torch.int32, "kept", nullable=True), ws, ws_n)
+
+
+# ---- steps whose rows, lengths and block lists are device data -------------------------------------
+def tide_rows_workspace_size(op: int, num_rows: int, dims: tide_dims, budget: int = 0, max_len: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().tide_rows_workspace_size(op, int(num_rows), int(budget), int(max_len), ctypes.byref(dims),
+                                           ctypes.byref(out)), "tide_rows_workspace_size")
+    return int(out.value)
+
+
+def _vector(t, name, n):
+    """t must be a 1-D tensor of n entries."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dim() != 1 or t.shape[0] != n:
+        raise ValueError("%s must have shape (%d,), got %s" % (name, n, tuple(t.shape)))
+
+
+def _count_of(t, name):
+    if not isinstance(t, torch.Tensor) or t.dim() != 1:
+        raise ValueError("%s must be a 1-D tensor" % name)
+    return t.shape[0]
+
+
+def _bounds_pools(bounds, units, num_pages, dims):
+    shape = (num_pages, dims.num_kv_heads, 2, dims.head_dim)
+    if tuple(bounds.shape) != shape:
+        raise ValueError("bounds must have shape %s, got %s" % (shape, tuple(bounds.shape)))
+    if tuple(units.shape) != shape[:2]:
+        raise ValueError("units must have shape %s, got %s" % (shape[:2], tuple(units.shape)))
+
+
+def tide_page_map(lens, want_lens, block_table, free_pages, free_count, lens_out, free_count_out, row_start,
+                  row_task, row_pos, row_slot, dims: tide_dims, stream=None) -> None:
+    """All of them device tensors: int32, row_slot int64."""
+    n, rows = _count_of(lens, "lens"), _count_of(row_task, "row_task")
+    for t, name, m in ((want_lens, "want_lens", n), (lens_out, "lens_out", n), (free_count, "free_count", 1),
+                       (free_count_out, "free_count_out", 1), (row_start, "row_start", n + 1),
+                       (row_pos, "row_pos", rows), (row_slot, "row_slot", rows)):
+        _vector(t, name, m)
+    stride = _block_table(block_table, n)
+    capacity = _count_of(free_pages, "free_pages")
+    _same_device(lens, want_lens, block_table, free_pages, free_count, lens_out, free_count_out, row_start,
+                 row_task, row_pos, row_slot)
+    i32 = torch.int32
+    _invoke("tide_page_map", lens, stream,
+            _dev(lens, i32, "lens"), _dev(want_lens, i32, "want_lens"), n, _dev(block_table, i32, "block_table"),
+            int(stride), _dev(free_pages, i32, "free_pages"), capacity, _dev(free_count, i32, "free_count"), rows,
+            _dev(lens_out, i32, "lens_out"), _dev(free_count_out, i32, "free_count_out"),
+            _dev(row_start, i32, "row_start"), _dev(row_task, i32, "row_task"), _dev(row_pos, i32, "row_pos"),
+            _dev(row_slot, torch.int64, "row_slot"), ctypes.byref(dims))
+
+
+def tide_slot_append(k_new, v_new, row_slot, k_pool, v_pool, dims: tide_dims, bounds=None, units=None,
+                     workspace=None, stream=None) -> None:
+    num_pages = _pool_shape(k_pool, v_pool, dims)
+    rows = _count_of(row_slot, "row_slot")
+    _rows(k_new, "k_new", rows, dims.num_kv_heads, dims.head_dim)
+    _rows(v_new, "v_new", rows, dims.num_kv_heads, dims.head_dim)
+    if (bounds is None) != (units is None):
+        raise ValueError("bounds and units go together")
+    if bounds is not None:
+        _bounds_pools(bounds, units, num_pages, dims)
+    _same_device(k_new, v_new, row_slot, k_pool, v_pool, bounds, units, workspace)
+    ws, ws_n = _ws(workspace)
+    _invoke("tide_slot_append", k_pool, stream,
+            _dev(k_new, torch.bfloat16, "k_new"), _dev(v_new, torch.bfloat16, "v_new"),
+            _dev(row_slot, torch.int64, "row_slot"), rows, _dev(k_pool, torch.bfloat16, "k_pool"),
+            _dev(v_pool, torch.bfloat16, "v_pool"), num_pages, _dev(bounds, torch.int8, "bounds", nullable=True),
+            _dev(units, torch.int8, "units", nullable=True), ctypes.byref(dims), ws, ws_n)
+
+
+def tide_key_bounds(k_pool, block_table, lens, bounds, units, dims: tide_dims, from_lens=None, max_len: int = 0,
+                    workspace=None, stream=None) -> None:
+    num_pages = _pool_shape(k_pool, k_pool, dims)
+    n = _count_of(lens, "lens")
+    if from_lens is not None:
+        _vector(from_lens, "from_lens", n)
+    _bounds_pools(bounds, units, num_pages, dims)
+    stride = _block_table(block_table, n)
+    _same_device(k_pool, block_table, lens, from_lens, bounds, units, workspace)
+    ws, ws_n = _ws(workspace)
+    _invoke("tide_key_bounds", k_pool, stream,
+            _dev(k_pool, torch.bfloat16, "k_pool"), num_pages, _dev(block_table, torch.int32, "block_table"),
+            int(stride), n, _dev(lens, torch.int32, "lens"), _dev(from_lens, torch.int32, "from_lens", nullable=True),
+            int(max_len), _dev(bounds, torch.int8, "bounds"), _dev(units, torch.int8, "units"), ctypes.byref(dims),
+            ws, ws_n)
+
+
+def tide_block_select(q, row_task, row_pos, bounds, units, block_table, budget: int, dims: tide_dims, sel,
+                      sink: int = 0, recent: int = 0, max_len: int = 0, workspace=None, stream=None) -> None:
+    rows = _count_of(row_task, "row_task")
+    _vector(row_pos, "row_pos", rows)
+    _rows(q, "q", rows, dims.num_q_heads, dims.head_dim)
+    num_pages = bounds.shape[0]
+    _bounds_pools(bounds, units, num_pages, dims)
+    if tuple(sel.shape) != (rows, dims.num_kv_heads, budget):
+        raise ValueError("sel must have shape (%d, %d, %d), got %s"
+                         % (rows, dims.num_kv_heads, budget, tuple(sel.shape)))
+    stride = _block_table(block_table, 0)
+    _same_device(q, row_task, row_pos, bounds, units, block_table, sel, workspace)
+    ws, ws_n = _ws(workspace)
+    _invoke("tide_block_select", q, stream,
+            _dev(q, torch.bfloat16, "q"), _dev(row_task, torch.int32, "row_task"),
+            _dev(row_pos, torch.int32, "row_pos"), rows, _dev(bounds, torch.int8, "bounds"),
+            _dev(units, torch.int8, "units"), num_pages, _dev(block_table, torch.int32, "block_table"),
+            int(stride), int(block_table.shape[0]), int(budget), int(sink), int(recent), int(max_len),
+            ctypes.byref(dims), _dev(sel, torch.int32, "sel"), ws, ws_n)
+
+
+def tide_sparse_attn(q, k_pool, v_pool, block_table, row_task, row_pos, sel, dims: tide_dims, out, lse=None,
+                     workspace=None, stream=None) -> None:
+    num_pages = _pool_shape(k_pool, v_pool, dims)
+    rows = _count_of(row_task, "row_task")
+    _vector(row_pos, "row_pos", rows)
+    _rows(q, "q", rows, dims.num_q_heads, dims.head_dim)
+    _rows(out, "out", rows, dims.num_q_heads, dims.head_dim)
+    _lse(lse, rows, dims.num_q_heads)
+    if sel.dim() != 3 or tuple(sel.shape[:2]) != (rows, dims.num_kv_heads):
+        raise ValueError("sel must be [%d][%d][budget], got %s" % (rows, dims.num_kv_heads, tuple(sel.shape)))
+    stride = _block_table(block_table, 0)
+    _same_device(q, k_pool, v_pool, block_table, row_task, row_pos, sel, out, lse, workspace)
+    ws, ws_n = _ws(workspace)
+    _invoke("tide_sparse_attn", k_pool, stream,
+            _dev(q, torch.bfloat16, "q"), _dev(k_pool, torch.bfloat16, "k_pool"),
+            _dev(v_pool, torch.bfloat16, "v_pool"), num_pages, _dev(block_table, torch.int32, "block_table"),
+            int(stride), int(block_table.shape[0]), _dev(row_task, torch.int32, "row_task"),
+            _dev(row_pos, torch.int32, "row_pos"), rows, _dev(sel, torch.int32, "sel"), int(sel.shape[2]),
+            ctypes.byref(dims), _dev(out, torch.bfloat16, "out"), _dev(lse, torch.float32, "lse", nullable=True),
+            ws, ws_n)
 
 
 def tide_shutdown() -> None:

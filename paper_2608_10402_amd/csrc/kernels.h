@@ -34,4 +34,13 @@ int kv4_store_groups(int32_t num_kv_heads);
 hipError_t launch_attn_mass(const MassArgs& a, int head_dim, bool kv4, hipStream_t stream);
 hipError_t launch_evict(const EvictArgs& a, int head_dim, bool kv4, hipStream_t stream);
 
+// Steps whose rows, lengths and block lists are device data.
+hipError_t launch_page_map(const PageMapArgs& a, hipStream_t stream);
+hipError_t launch_slot_append(const SlotAppendArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_key_bounds(const KeyBoundsArgs& a, int head_dim, int32_t num_tasks, hipStream_t stream);
+hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_sparse(const SparseArgs& a, int head_dim, bool shared, hipStream_t stream);
+// Query rows that a wave of the score kernel takes at once.
+int select_tile_rows(int32_t group, bool chunk);
+
 }  // namespace tide

@@ -1,0 +1,343 @@
+// The extern "C" entry points of steps whose rows, lengths and block lists are device data
+// (include/tide.h): checks, workspaces, launches.  Nothing is planned from lengths, so nothing is staged.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "kernels.h"
+#include "plan.h"
+#include "staging.h"
+#include "tide.h"
+
+namespace tide {
+namespace {
+
+constexpr size_t kHeader = sizeof(WsHeader);
+
+bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Checks that the entry points of rows start with.  *go: there is something to do.
+int begin(const tide_dims* dims, int32_t count, int64_t num_pages, bool* go) {
+  *go = false;
+  const int rc = check_dims(dims);
+  if (rc != TIDE_OK) return rc;
+  if (count < 0) return TIDE_ERR_INVALID_ARG;
+  if (count == 0) return TIDE_OK;
+  if (num_pages <= 0) return TIDE_ERR_INVALID_ARG;
+  *go = true;
+  return TIDE_OK;
+}
+
+// The longest context of a call: max_len, or (0) all that the block table holds.
+int longest(int32_t max_len, int32_t bt_stride, int32_t* out) {
+  const int64_t most = std::min<int64_t>((int64_t)bt_stride * kPage, INT32_MAX);
+  if (max_len < 0) return TIDE_ERR_INVALID_ARG;
+  if (max_len > most) return TIDE_ERR_CAPACITY;
+  *out = max_len ? max_len : (int32_t)most;
+  return TIDE_OK;
+}
+
+// ---- selection: rows go in rounds of at most kScoreBytes of scores, which stay in the last-level cache
+constexpr int64_t kScoreBytes = 256 << 20;
+constexpr int32_t kRoundPairs = 1 << 20;  // (row, kv head) pairs of a round
+constexpr int64_t kScoreWaves = 8192;     // waves of the score kernel: twice what the device holds
+
+struct SelectRounds {
+  int32_t rows;         // of a round
+  int32_t stride;       // scores of a (row, kv head)
+  size_t bytes;
+};
+
+SelectRounds select_rounds(int32_t num_rows, int32_t max_len, const tide_dims& dims) {
+  SelectRounds r;
+  const int64_t blocks = ((int64_t)max_len + kPage - 1) / kPage;
+  r.stride = (int32_t)((blocks + 15) / 16 * 16);
+  const int64_t row = (int64_t)r.stride * dims.num_kv_heads * 4;
+  const int64_t most = std::min<int64_t>(kScoreBytes / row, kRoundPairs / dims.num_kv_heads);
+  r.rows = (int32_t)std::min<int64_t>(num_rows, std::max<int64_t>(1, most));
+  r.bytes = kHeader + (size_t)((int64_t)r.rows * row);
+  return r;
+}
+
+// ---- sparse attention: workgroups that share a (row, kv head) where there are few of them
+constexpr int32_t kSparseGroups = 512;     // that the device holds at once
+constexpr int32_t kLeastPairs = 8;         // pairs of blocks of a workgroup: two a wave
+constexpr int32_t kSparseLaunch = 1 << 23; // workgroups of a launch (fewer than 2^32 threads)
+
+int32_t sparse_splits(int64_t num_rows, int32_t budget, const tide_dims& dims) {
+  const int64_t units = num_rows * dims.num_kv_heads;
+  const int64_t pairs = ((int64_t)budget + 1) / 2;
+  return (int32_t)std::max<int64_t>(1, std::min(kSparseGroups / units, pairs / kLeastPairs));
+}
+
+size_t sparse_bytes(int32_t num_rows, int32_t budget, const tide_dims& dims, size_t* ml_off) {
+  const int64_t splits = sparse_splits(num_rows, budget, dims);
+  if (splits == 1) return kHeader;
+  const size_t rows = (size_t)num_rows * dims.num_q_heads * splits;  // at most 512 x 16
+  *ml_off = kHeader + rows * dims.head_dim * 4;
+  return *ml_off + rows * 16;
+}
+
+}  // namespace
+}  // namespace tide
+
+using namespace tide;
+
+extern "C" {
+
+TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, int32_t max_len, const tide_dims* dims,
+                                      size_t* bytes_out) {
+  try {
+    const int rc = check_dims(dims);
+    if (rc != TIDE_OK) return rc;
+    if (!bytes_out || num_rows < 0) return TIDE_ERR_INVALID_ARG;
+    size_t ml_off = 0;
+    switch (op) {
+      case TIDE_OP_SLOT_APPEND:
+      case TIDE_OP_KEY_BOUNDS:
+        *bytes_out = kHeader;
+        return TIDE_OK;
+      case TIDE_OP_BLOCK_SELECT:
+        if (max_len <= 0) return TIDE_ERR_INVALID_ARG;
+        *bytes_out = num_rows ? select_rounds(num_rows, max_len, *dims).bytes : kHeader;
+        return TIDE_OK;
+      case TIDE_OP_SPARSE_ATTN:
+        if (budget <= 0) return TIDE_ERR_INVALID_ARG;
+        *bytes_out = num_rows ? sparse_bytes(num_rows, budget, *dims, &ml_off) : kHeader;
+        return TIDE_OK;
+      default:
+        return TIDE_ERR_INVALID_ARG;
+    }
+  } catch (...) {
+    return TIDE_ERR_HIP;
+  }
+}
+
+TIDE_API int tide_page_map(const int32_t* lens, const int32_t* want_lens, int32_t num_tasks, int32_t* block_table,
+                           int32_t bt_stride, int32_t* free_pages, int32_t free_capacity, const int32_t* free_count,
+                           int32_t num_rows, int32_t* lens_out, int32_t* free_count_out, int32_t* row_start,
+                           int32_t* row_task, int32_t* row_pos, int64_t* row_slot, const tide_dims* dims, void* stream) {
+  try {
+    const int rc = check_dims(dims);
+    if (rc != TIDE_OK) return rc;
+    if (num_tasks < 0 || num_rows < 0 || free_capacity < 0) return TIDE_ERR_INVALID_ARG;
+    if (num_tasks == 0) return TIDE_OK;
+    if (bt_stride <= 0) return TIDE_ERR_INVALID_ARG;
+    if ((int64_t)num_tasks * bt_stride > INT32_MAX || num_rows == INT32_MAX) return TIDE_ERR_UNSUPPORTED;
+    if (!lens || !want_lens || !block_table || !free_count || !lens_out || !free_count_out || !row_start ||
+        (free_capacity > 0 && !free_pages) || (num_rows > 0 && (!row_task || !row_pos || !row_slot)))
+      return TIDE_ERR_INVALID_ARG;
+    PageMapArgs a = {};
+    a.lens = lens;
+    a.want = want_lens;
+    a.num_tasks = num_tasks;
+    a.block_table = block_table;
+    a.bt_stride = bt_stride;
+    a.free_pages = free_pages;
+    a.capacity = free_capacity;
+    a.free_count = free_count;
+    a.num_rows = num_rows;
+    a.lens_out = lens_out;
+    a.free_count_out = free_count_out;
+    a.row_start = row_start;
+    a.row_task = row_task;
+    a.row_pos = row_pos;
+    a.row_slot = row_slot;
+    return launch_page_map(a, static_cast<hipStream_t>(stream)) == hipSuccess ? TIDE_OK : TIDE_ERR_HIP;
+  } catch (...) {
+    return TIDE_ERR_HIP;
+  }
+}
+
+TIDE_API int tide_slot_append(const void* k_new, const void* v_new, const int64_t* row_slot, int32_t num_rows,
+                              void* k_pool, void* v_pool, int64_t num_pages, int8_t* bounds, int8_t* units,
+                              const tide_dims* dims, void* workspace, size_t workspace_bytes, void* stream) {
+  try {
+    bool go;
+    int rc = begin(dims, num_rows, num_pages, &go);
+    if (rc != TIDE_OK || !go) return rc;
+    if (!k_new || !v_new || !row_slot || !k_pool || !v_pool || !workspace || !bounds != !units)
+      return TIDE_ERR_INVALID_ARG;
+    if (!on16(k_new) || !on16(v_new) || !on16(k_pool) || !on16(v_pool) || !on16(bounds) || !on16(workspace))
+      return TIDE_ERR_INVALID_ARG;
+    if (workspace_bytes < kHeader) return TIDE_ERR_CAPACITY;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = clear_flags(workspace, s);
+    if (rc != TIDE_OK) return rc;
+    SlotAppendArgs a = {};
+    a.k_new = static_cast<const uint16_t*>(k_new);
+    a.v_new = static_cast<const uint16_t*>(v_new);
+    a.row_slot = row_slot;
+    a.k_pool = static_cast<uint16_t*>(k_pool);
+    a.v_pool = static_cast<uint16_t*>(v_pool);
+    a.num_pages = num_pages;
+    a.num_kv_heads = dims->num_kv_heads;
+    a.num_rows = num_rows;
+    a.bounds = bounds;
+    a.units = units;
+    a.error_flags = at_mut<int32_t>(workspace, 0);
+    Staged none;
+    return finish(launch_slot_append(a, dims->head_dim, s), none, workspace, s);
+  } catch (...) {
+    return TIDE_ERR_HIP;
+  }
+}
+
+TIDE_API int tide_key_bounds(const void* k_pool, int64_t num_pages, const int32_t* block_table, int32_t bt_stride,
+                             int32_t num_tasks, const int32_t* lens, const int32_t* from_lens, int32_t max_len,
+                             int8_t* bounds, int8_t* units, const tide_dims* dims, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  try {
+    bool go;
+    int rc = begin(dims, num_tasks, num_pages, &go);
+    if (rc != TIDE_OK || !go) return rc;
+    if (bt_stride <= 0) return TIDE_ERR_INVALID_ARG;
+    int32_t most;
+    rc = longest(max_len, bt_stride, &most);
+    if (rc != TIDE_OK) return rc;
+    if (!k_pool || !block_table || !lens || !bounds || !units || !workspace) return TIDE_ERR_INVALID_ARG;
+    if (!on16(k_pool) || !on16(bounds) || !on16(workspace)) return TIDE_ERR_INVALID_ARG;
+    if (workspace_bytes < kHeader) return TIDE_ERR_CAPACITY;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = clear_flags(workspace, s);
+    if (rc != TIDE_OK) return rc;
+    KeyBoundsArgs a = {};
+    a.k_pool = static_cast<const uint16_t*>(k_pool);
+    a.num_pages = num_pages;
+    a.block_table = block_table;
+    a.bt_stride = bt_stride;
+    a.num_kv_heads = dims->num_kv_heads;
+    a.lens = lens;
+    a.from = from_lens;
+    a.max_len = most;
+    a.bounds = bounds;
+    a.units = units;
+    a.error_flags = at_mut<int32_t>(workspace, 0);
+    Staged none;
+    return finish(launch_key_bounds(a, dims->head_dim, num_tasks, s), none, workspace, s);
+  } catch (...) {
+    return TIDE_ERR_HIP;
+  }
+}
+
+TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int32_t* row_pos, int32_t num_rows,
+                               const int8_t* bounds, const int8_t* units, int64_t num_pages,
+                               const int32_t* block_table, int32_t bt_stride, int32_t num_tasks, int32_t budget,
+                               int32_t sink, int32_t recent, int32_t max_len, const tide_dims* dims, int32_t* sel,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+  try {
+    bool go;
+    int rc = begin(dims, num_rows, num_pages, &go);
+    if (rc != TIDE_OK) return rc;
+    if (budget <= 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > budget || num_tasks < 0)
+      return TIDE_ERR_INVALID_ARG;
+    if (!go || num_tasks == 0) return TIDE_OK;
+    if (bt_stride <= 0) return TIDE_ERR_INVALID_ARG;
+    int32_t most;
+    rc = longest(max_len, bt_stride, &most);
+    if (rc != TIDE_OK) return rc;
+    if (!q || !row_task || !row_pos || !bounds || !units || !block_table || !sel || !workspace)
+      return TIDE_ERR_INVALID_ARG;
+    if (!on16(q) || !on16(bounds) || !on16(workspace)) return TIDE_ERR_INVALID_ARG;
+    const SelectRounds rounds = select_rounds(num_rows, most, *dims);
+    if (workspace_bytes < rounds.bytes) return TIDE_ERR_CAPACITY;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = clear_flags(workspace, s);
+    if (rc != TIDE_OK) return rc;
+    BlockSelectArgs a = {};
+    a.q = static_cast<const uint16_t*>(q);
+    a.row_task = row_task;
+    a.row_pos = row_pos;
+    a.bounds = bounds;
+    a.units = units;
+    a.num_pages = num_pages;
+    a.block_table = block_table;
+    a.bt_stride = bt_stride;
+    a.num_tasks = num_tasks;
+    a.num_q_heads = dims->num_q_heads;
+    a.num_kv_heads = dims->num_kv_heads;
+    a.group = dims->num_q_heads / dims->num_kv_heads;
+    a.max_len = most;
+    a.scores = at_mut<float>(workspace, kHeader);
+    a.score_stride = rounds.stride;
+    a.budget = budget;
+    a.sink = sink;
+    a.recent = recent;
+    a.sel = sel;
+    a.error_flags = at_mut<int32_t>(workspace, 0);
+    // one row a task: nothing to share between rows; more: rows of a task go together
+    a.tile_rows = select_tile_rows(a.group, num_rows > num_tasks);
+    hipError_t err = hipSuccess;
+    for (int64_t first = 0; first < num_rows && err == hipSuccess; first += rounds.rows) {
+      a.first_row = (int32_t)first;
+      a.rows = (int32_t)std::min<int64_t>(rounds.rows, num_rows - first);
+      const int64_t waves = (int64_t)((a.rows + a.tile_rows - 1) / a.tile_rows) * a.num_kv_heads;
+      a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>((kScoreWaves + waves - 1) / waves, (rounds.stride + 63) / 64));
+      err = launch_block_select(a, dims->head_dim, s);
+    }
+    Staged none;
+    return finish(err, none, workspace, s);
+  } catch (...) {
+    return TIDE_ERR_HIP;
+  }
+}
+
+TIDE_API int tide_sparse_attn(const void* q, const void* k_pool, const void* v_pool, int64_t num_pages,
+                              const int32_t* block_table, int32_t bt_stride, int32_t num_tasks,
+                              const int32_t* row_task, const int32_t* row_pos, int32_t num_rows, const int32_t* sel,
+                              int32_t budget, const tide_dims* dims, void* out, float* lse, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  try {
+    bool go;
+    int rc = begin(dims, num_rows, num_pages, &go);
+    if (rc != TIDE_OK) return rc;
+    if (budget <= 0 || num_tasks < 0) return TIDE_ERR_INVALID_ARG;
+    if (!go || num_tasks == 0) return TIDE_OK;
+    if (bt_stride <= 0) return TIDE_ERR_INVALID_ARG;
+    if (!q || !k_pool || !v_pool || !block_table || !row_task || !row_pos || !sel || !out || !workspace)
+      return TIDE_ERR_INVALID_ARG;
+    if (!on16(q) || !on16(k_pool) || !on16(v_pool) || !on16(out) || !on16(workspace)) return TIDE_ERR_INVALID_ARG;
+    size_t ml_off = 0;
+    if (workspace_bytes < sparse_bytes(num_rows, budget, *dims, &ml_off)) return TIDE_ERR_CAPACITY;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = clear_flags(workspace, s);
+    if (rc != TIDE_OK) return rc;
+    SparseArgs a = {};
+    a.q = static_cast<const uint16_t*>(q);
+    a.k_pool = static_cast<const uint16_t*>(k_pool);
+    a.v_pool = static_cast<const uint16_t*>(v_pool);
+    a.num_pages = num_pages;
+    a.block_table = block_table;
+    a.bt_stride = bt_stride;
+    a.num_tasks = num_tasks;
+    a.num_q_heads = dims->num_q_heads;
+    a.num_kv_heads = dims->num_kv_heads;
+    a.group = dims->num_q_heads / dims->num_kv_heads;
+    a.scale_log2 = dims->sm_scale * 1.44269504088896340736f;
+    a.row_task = row_task;
+    a.row_pos = row_pos;
+    a.sel = sel;
+    a.budget = budget;
+    a.splits = sparse_splits(num_rows, budget, *dims);
+    a.part_o = at_mut<float>(workspace, kHeader);
+    a.part_ml = at_mut<float>(workspace, ml_off);
+    a.out = static_cast<uint16_t*>(out);
+    a.lse = lse;
+    a.error_flags = at_mut<int32_t>(workspace, 0);
+    // rows of one task share pages; a row of its own streams them
+    const bool shared = num_rows > num_tasks;
+    const int64_t most = std::max<int64_t>(1, kSparseLaunch / ((int64_t)a.num_kv_heads * a.splits));
+    hipError_t err = hipSuccess;
+    for (int64_t first = 0; first < num_rows && err == hipSuccess; first += most) {
+      a.first_row = (int32_t)first;
+      a.rows = (int32_t)std::min<int64_t>(most, num_rows - first);
+      err = launch_sparse(a, dims->head_dim, shared, s);
+    }
+    Staged none;
+    return finish(err, none, workspace, s);
+  } catch (...) {
+    return TIDE_ERR_HIP;
+  }
+}
+
+}  // extern "C"

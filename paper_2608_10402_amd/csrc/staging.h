@@ -40,6 +40,9 @@ int upload(const Plan& plan, void* workspace, hipStream_t stream, uint32_t reade
 // checks waits for the stream and reads the workspace's error flags.
 int finish(hipError_t launch_status, Staged& st, void* workspace, hipStream_t stream);
 
+// Starts a call without a plan: under debug checks its workspace's error flags are cleared.
+int clear_flags(void* workspace, hipStream_t stream);
+
 // An extend of a plan made with its work lists: everything behind the arguments' checks.
 int run_extend_plan(const Plan& plan, const void* q, const void* k_pool, const void* v_pool, int64_t num_pages,
                     const int32_t* block_table, int32_t bt_stride, const tide_dims& dims, void* out, float* lse,

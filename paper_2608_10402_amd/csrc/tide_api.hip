@@ -276,6 +276,14 @@ int finish(hipError_t launch_status, Staged& st, void* workspace, hipStream_t st
   return (flags & 1) ? TIDE_ERR_PAGE_RANGE : TIDE_OK;
 }
 
+int clear_flags(void* workspace, hipStream_t stream) {
+  if (!debug_checks()) return TIDE_OK;
+  static_assert(sizeof(WsHeader) % 16 == 0, "16 bytes a thread");
+  hipLaunchKernelGGL(zero_kernel, dim3(1), dim3(256), 0, stream, static_cast<u32x4_t*>(workspace),
+                     (uint32_t)(sizeof(WsHeader) / 16));
+  return hipGetLastError() == hipSuccess ? TIDE_OK : TIDE_ERR_HIP;
+}
+
 uint64_t next_call() {
   static std::atomic<uint64_t> count([] {
     std::random_device r;

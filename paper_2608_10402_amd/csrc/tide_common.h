@@ -502,4 +502,115 @@ struct EvictArgs {
   PlanReads reads;
 };
 
+// ---- steps whose rows, lengths and block lists are device data -------------------------------------
+// A row is one query token: its task (block-table row) and its position in it; either negative, or out
+// of range, marks a row that nothing is done for.
+TIDE_HD inline bool live_row(int32_t task, int32_t pos, int32_t num_tasks, int64_t max_len) {
+  return task >= 0 && task < num_tasks && pos >= 0 && pos < max_len;
+}
+
+struct PageMapArgs {
+  const int32_t* lens;
+  const int32_t* want;
+  int32_t num_tasks;
+  int32_t* block_table;
+  int32_t bt_stride;
+  int32_t* free_pages;  // a stack
+  int32_t capacity;
+  const int32_t* free_count;
+  int32_t num_rows;
+  int32_t* lens_out;
+  int32_t* free_count_out;
+  int32_t* row_start;  // [num_tasks + 1]
+  int32_t* row_task;   // [num_rows] each
+  int32_t* row_pos;
+  int64_t* row_slot;
+  bool rows_apart;     // the rows are written by a kernel of their own
+};
+
+// Key bounds: per (page, kv head) d upper and d lower bounds in whole units 2^units (kNoUnit: a key
+// of the page is not finite).
+constexpr int kLeastUnit = -120, kMostUnit = 122, kNoUnit = 127;
+
+struct SlotAppendArgs {
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  const int64_t* row_slot;
+  uint16_t* k_pool;
+  uint16_t* v_pool;
+  int64_t num_pages;
+  int32_t num_kv_heads;
+  int32_t num_rows;
+  int32_t first_row, rows;  // of the launch
+  int8_t* bounds;           // [num_pages][Hkv][2][d], may be null
+  int8_t* units;            // [num_pages][Hkv]
+  int32_t* error_flags;
+};
+
+struct KeyBoundsArgs {
+  const uint16_t* k_pool;
+  int64_t num_pages;
+  const int32_t* block_table;
+  int32_t bt_stride;
+  int32_t num_kv_heads;
+  const int32_t* lens;
+  const int32_t* from;  // may be null: 0
+  int32_t max_len;
+  int32_t chunks;       // of a task: the pages of one wave
+  int32_t first_task, first_chunk, units_here;  // (task, chunk) pairs of the launch
+  int8_t* bounds;
+  int8_t* units;
+  int32_t* error_flags;
+};
+
+struct BlockSelectArgs {
+  const uint16_t* q;
+  const int32_t* row_task;
+  const int32_t* row_pos;
+  const int8_t* bounds;
+  const int8_t* units;
+  int64_t num_pages;
+  const int32_t* block_table;
+  int32_t bt_stride;
+  int32_t num_tasks;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t group;
+  int32_t max_len;
+  int32_t first_row, rows;  // of the launches
+  int32_t tile_rows;        // rows of a unit of the score kernel
+  int32_t splits;           // waves that share a (unit, kv head)
+  float* scores;            // [rows][Hkv][score_stride]
+  int32_t score_stride;     // blocks, a multiple of 16
+  int32_t budget, sink, recent;
+  int32_t* sel;             // [num_rows][Hkv][budget]
+  int32_t* error_flags;
+};
+
+struct SparseArgs {
+  const uint16_t* q;
+  const uint16_t* k_pool;
+  const uint16_t* v_pool;
+  int64_t num_pages;
+  const int32_t* block_table;
+  int32_t bt_stride;
+  int32_t num_tasks;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t group;
+  float scale_log2;
+  const int32_t* row_task;
+  const int32_t* row_pos;
+  int32_t first_row, rows;  // of the launch
+  const int32_t* sel;
+  int32_t budget;
+  int32_t splits;       // workgroups that share a (row, kv head)
+  float* part_o;        // [rows of a launch][Hkv][splits][group][d]
+  float* part_ml;       // [..][splits][group][4]: max (base-2 units), sum of the bf16-rounded weights,
+                        // exact sum, 1 if the part has a key
+  uint16_t* out;
+  float* lse;
+  int32_t* error_flags;
+};
+
 }  // namespace tide

@@ -1,5 +1,6 @@
 """Paged KV pools on one device with the entry points bound to them: `PagedKV` holds K and V in
-bf16, `PagedKV4` in 4 bits.
+bf16, `PagedKV4` in 4 bits.  `PageTable` is a block table whose lengths and free pages live on the
+device too.
 
 Convenience layer over the C ABI: owns the page pools, the block table and a
 grow-only workspace, and forwards each call to libtide.so.  No arithmetic happens here.
@@ -187,6 +188,87 @@ class PagedKV(_Paged):
         pages: make it the block table (`block_table = ...`) to go on with them."""
         return self._evict(lambda *a: _lib.tide_kv_evict(self.k_pool, self.v_pool, *a), mass, kv_lens,
                            keep_lens, recent_lens, new_block_table, kept, stream)
+
+
+    # ---- steps whose rows, lengths and block lists are device data.  A call that is captured into a
+    # graph keeps this object's workspace, which a later, larger call replaces: give a graph a PagedKV of
+    # its own over the same pools, or make its calls once before the capture and no larger ones after.
+
+    def new_bounds(self):
+        """Key bounds for append_slots, key_bounds and select_blocks: (bounds, units) of every page."""
+        shape = (self.num_pages, self.dims.num_kv_heads, 2, self.dims.head_dim)
+        return (torch.zeros(shape, dtype=torch.int8, device=self.device),
+                torch.zeros(shape[:2], dtype=torch.int8, device=self.device))
+
+    def append_slots(self, k_new, v_new, row_slot, bounds=None, stream=None):
+        """Store the rows' K/V in their slots (tide_slot_append); with bounds, bring those of the
+        pages that change up to date."""
+        b, u = bounds if bounds is not None else (None, None)
+        self._call(lambda: _lib.tide_rows_workspace_size(_lib.TIDE_OP_SLOT_APPEND, row_slot.numel(), self.dims),
+                   lambda ws: _lib.tide_slot_append(k_new, v_new, row_slot, self.k_pool, self.v_pool, self.dims, b, u,
+                                                    ws, stream))
+
+    def key_bounds(self, lens, bounds, from_lens=None, max_len: int = 0, stream=None):
+        """Key bounds of the pages that hold positions from_lens (None: 0) .. lens - 1 of each task, both on
+        the device (tide_key_bounds): after append, extend_append, evict and what else writes keys."""
+        self._call(lambda: _lib.tide_rows_workspace_size(_lib.TIDE_OP_KEY_BOUNDS, lens.numel(), self.dims),
+                   lambda ws: _lib.tide_key_bounds(self.k_pool, self.block_table, lens, bounds[0], bounds[1],
+                                                   self.dims, from_lens, max_len, ws, stream))
+        return bounds
+
+    def select_blocks(self, q, row_task, row_pos, bounds, budget: int, sink: int = 0, recent: int = 0,
+                      max_len: int = 0, out=None, stream=None):
+        """The `budget` blocks that each row and kv head attends to (tide_block_select), int32
+        [rows][Hkv][budget]; those of padding rows are not written."""
+        if out is None:
+            out = torch.empty((q.shape[0], self.dims.num_kv_heads, budget), dtype=torch.int32, device=q.device)
+        longest = max_len if max_len > 0 else min(self.block_table.shape[1] * self.dims.page_size, 2**31 - 1)
+        self._call(lambda: _lib.tide_rows_workspace_size(_lib.TIDE_OP_BLOCK_SELECT, q.shape[0], self.dims,
+                                                         max_len=longest),
+                   lambda ws: _lib.tide_block_select(q, row_task, row_pos, bounds[0], bounds[1], self.block_table,
+                                                     budget, self.dims, out, sink, recent, max_len, ws, stream))
+        return out
+
+    def sparse(self, q, row_task, row_pos, sel, out=None, lse=None, stream=None):
+        """Attention of each row over the blocks in sel (tide_sparse_attn); padding rows are not
+        written."""
+        out = torch.empty_like(q) if out is None else out
+        self._call(lambda: _lib.tide_rows_workspace_size(_lib.TIDE_OP_SPARSE_ATTN, q.shape[0], self.dims,
+                                                         budget=sel.shape[2]),
+                   lambda ws: _lib.tide_sparse_attn(q, self.k_pool, self.v_pool, self.block_table, row_task, row_pos,
+                                                    sel, self.dims, out, lse, ws, stream))
+        return out
+
+
+class PageTable:
+    """Block table, lengths and free pages of num_tasks tasks on the device, changed by `map` alone, so
+    that a step (captured or not) needs no lengths from the host.  pages: how many there are, or the
+    ids that are free.  Use `block_table` as a PagedKV's: `kv.block_table = table.block_table`."""
+
+    def __init__(self, num_tasks: int, pages_per_task: int, pages, device="cuda"):
+        self.device = torch.device(device)
+        # the lowest ids on top of the stack
+        ids = np.arange(pages)[::-1] if np.ndim(pages) == 0 else np.asarray(pages)
+        self.free_pages = torch.from_numpy(np.ascontiguousarray(ids, dtype=np.int32)).to(self.device)
+        self.free_count = torch.full((1,), self.free_pages.numel(), dtype=torch.int32, device=self.device)
+        self.block_table = torch.zeros((num_tasks, pages_per_task), dtype=torch.int32, device=self.device)
+        self.lens = torch.zeros(num_tasks, dtype=torch.int32, device=self.device)
+        self.row_start = torch.zeros(num_tasks + 1, dtype=torch.int32, device=self.device)
+        self._dims = _lib.make_dims(1, 1, 64, 1.0)  # (the page size)
+
+    def new_rows(self, num_rows: int):
+        """(row_task, row_pos, row_slot) for `map`, all padding."""
+        return (torch.full((num_rows,), -1, dtype=torch.int32, device=self.device),
+                torch.full((num_rows,), -1, dtype=torch.int32, device=self.device),
+                torch.full((num_rows,), -1, dtype=torch.int64, device=self.device))
+
+    def map(self, want_lens, rows, stream=None):
+        """Bring every task's length to want_lens (device int32 [num_tasks]), taking pages or giving them
+        back (tide_page_map), and put the new tokens into rows (from new_rows).  A task that is refused
+        keeps its length: lens != want_lens."""
+        _lib.tide_page_map(self.lens, want_lens, self.block_table, self.free_pages, self.free_count, self.lens,
+                           self.free_count, self.row_start, rows[0], rows[1], rows[2], self._dims, stream)
+        return rows
 
 
 class PagedKV4(_Paged):
