@@ -40,7 +40,8 @@ int longest(int32_t max_len, int32_t bt_stride, int32_t* out) {
 // ---- selection: rows go in rounds of at most kScoreBytes of scores, which stay in the last-level cache
 constexpr int64_t kScoreBytes = 256 << 20;
 constexpr int32_t kRoundPairs = 1 << 20;  // (row, kv head) pairs of a round
-constexpr int64_t kScoreWaves = 8192;     // waves of the score kernel: twice what the device holds
+// Waves of the score kernels: contexts differ, so rows are cut finer than the device needs to be full.
+constexpr int64_t kScoreRowWaves = 8192, kScoreChunkWaves = 4096;
 
 struct SelectRounds {
   int32_t rows;         // of a round
@@ -51,7 +52,7 @@ struct SelectRounds {
 SelectRounds select_rounds(int32_t num_rows, int32_t max_len, const tide_dims& dims) {
   SelectRounds r;
   const int64_t blocks = ((int64_t)max_len + kPage - 1) / kPage;
-  r.stride = (int32_t)((blocks + 15) / 16 * 16);
+  r.stride = (int32_t)((blocks + kScoreChunk - 1) / kScoreChunk * kScoreChunk);
   const int64_t row = (int64_t)r.stride * dims.num_kv_heads * 4;
   const int64_t most = std::min<int64_t>(kScoreBytes / row, kRoundPairs / dims.num_kv_heads);
   r.rows = (int32_t)std::min<int64_t>(num_rows, std::max<int64_t>(1, most));
@@ -258,7 +259,7 @@ TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int
     a.num_kv_heads = dims->num_kv_heads;
     a.group = dims->num_q_heads / dims->num_kv_heads;
     a.max_len = most;
-    a.scores = at_mut<float>(workspace, kHeader);
+    a.scores = at_mut<int32_t>(workspace, kHeader);
     a.score_stride = rounds.stride;
     a.budget = budget;
     a.sink = sink;
@@ -267,12 +268,13 @@ TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int
     a.error_flags = at_mut<int32_t>(workspace, 0);
     // one row a task: nothing to share between rows; more: rows of a task go together
     a.tile_rows = select_tile_rows(a.group, num_rows > num_tasks);
+    const int64_t target = a.tile_rows == 1 ? kScoreRowWaves : kScoreChunkWaves;
     hipError_t err = hipSuccess;
     for (int64_t first = 0; first < num_rows && err == hipSuccess; first += rounds.rows) {
       a.first_row = (int32_t)first;
       a.rows = (int32_t)std::min<int64_t>(rounds.rows, num_rows - first);
       const int64_t waves = (int64_t)((a.rows + a.tile_rows - 1) / a.tile_rows) * a.num_kv_heads;
-      a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>((kScoreWaves + waves - 1) / waves, (rounds.stride + 63) / 64));
+      a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>((target + waves - 1) / waves, rounds.stride / kScoreChunk));
       err = launch_block_select(a, dims->head_dim, s);
     }
     Staged none;

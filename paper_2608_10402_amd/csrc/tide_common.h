@@ -563,6 +563,9 @@ struct KeyBoundsArgs {
   int32_t* error_flags;
 };
 
+// Blocks that a wave of the score kernel takes at a time, one page id a lane.
+constexpr int kScoreChunk = 64;
+
 struct BlockSelectArgs {
   const uint16_t* q;
   const int32_t* row_task;
@@ -580,8 +583,8 @@ struct BlockSelectArgs {
   int32_t first_row, rows;  // of the launches
   int32_t tile_rows;        // rows of a unit of the score kernel
   int32_t splits;           // waves that share a (unit, kv head)
-  float* scores;            // [rows][Hkv][score_stride]
-  int32_t score_stride;     // blocks, a multiple of 16
+  int32_t* scores;          // [rows][Hkv][score_stride], integers that order like the scores
+  int32_t score_stride;     // blocks, a multiple of kScoreChunk
   int32_t budget, sink, recent;
   int32_t* sel;             // [num_rows][Hkv][budget]
   int32_t* error_flags;
