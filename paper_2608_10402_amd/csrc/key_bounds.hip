@@ -25,6 +25,7 @@ namespace kern {
 typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBoundWaves = 4;
+constexpr int64_t kAppendWaves = 16384;
 
 // One page's rows as its wave loads them: lane l has piece l % kG of rows l / kG + kRows i.
 template <int D>
@@ -46,119 +47,148 @@ __device__ __forceinline__ float value_of(int16_t o) {
   return __builtin_bit_cast(float, (uint32_t)b << 16);
 }
 
-__device__ __forceinline__ i16x2 shfl_i16x2(i16x2 v, int mask) {
-  return __builtin_bit_cast(i16x2, __shfl_xor(__builtin_bit_cast(int, v), mask, 64));
+// Lane groups of 16 (or halves): the larger of a's pair of groups in one, of b's in the other (max_groups, max_halves
+// of block_select.hip, two entries at a time); kMin: the smaller.
+template <bool kMin>
+__device__ __forceinline__ uint32_t pick(uint32_t a, uint32_t b) {
+  const i16x2 x = __builtin_bit_cast(i16x2, a), y = __builtin_bit_cast(i16x2, b);
+  return __builtin_bit_cast(uint32_t, kMin ? __builtin_elementwise_min(x, y) : __builtin_elementwise_max(x, y));
 }
 
-// Bounds of the first n (1 .. 16) rows, stored for (page, head) = block `at` of the pools.
+template <bool kMin>
+__device__ __forceinline__ uint32_t join16(uint32_t a, uint32_t b) {
+  const auto s = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  return pick<kMin>((uint32_t)s[0], (uint32_t)s[1]);
+}
+
+template <bool kMin>
+__device__ __forceinline__ uint32_t join32(uint32_t a, uint32_t b) {
+  const auto s = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return pick<kMin>((uint32_t)s[0], (uint32_t)s[1]);
+}
+
+// Over the wave's row groups: lane l gets the word of entries 8 (l % kG) + 2 (l / 16) of x[0 .. 3].
+template <int D, bool kMin>
+__device__ __forceinline__ uint32_t over_rows(const uint32_t (&x)[4]) {
+  uint32_t y = join32<kMin>(join16<kMin>(x[0], x[1]), join16<kMin>(x[2], x[3]));
+  if (D == 64) y = pick<kMin>(y, (uint32_t)__builtin_amdgcn_mov_dpp((int)y, 0x128, 0xF, 0xF, true));  // row_ror:8
+  return y;
+}
+
+// The largest of the wave's x.
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x121, 0xF, 0xF, true));  // row_ror 1, 2, 4, 8: over 16 lanes
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x122, 0xF, 0xF, true));
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x124, 0xF, 0xF, true));
+  x = max(x, __builtin_amdgcn_mov_dpp(x, 0x128, 0xF, 0xF, true));
+  const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+  x = max((int)r[0], (int)r[1]);
+  const auto h = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+  return max((int)h[0], (int)h[1]);
+}
+
+// Bounds of a page's rows, stored for (page, head) = block `at` of the pools.  Rows past the last position repeat
+// one that counts.
 template <int D>
-__device__ __forceinline__ void put_bounds(const PageRows<D>& rows, int n, int8_t* bounds, int8_t* units, int64_t at) {
+__device__ __forceinline__ void put_bounds(const PageRows<D>& rows, int8_t* bounds, int8_t* units, int64_t at) {
   using R = PageRows<D>;
-  const int lane = threadIdx.x & 63, part = lane % R::kG, row = lane / R::kG;
-  constexpr int16_t kInf = 0x7F80;
-  i16x2 hi[4], lo[4];
+  const int lane = threadIdx.x & 63, part = lane % R::kG;
+  constexpr int kInf = 0x7F80;
+  uint32_t hi[4], lo[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    hi[j] = i16x2{INT16_MIN, INT16_MIN};
-    lo[j] = i16x2{INT16_MAX, INT16_MAX};
-  }
+    hi[j] = lo[j] = __builtin_bit_cast(uint32_t, ordered(rows.x[0][j]));
 #pragma unroll
-  for (int i = 0; i < R::kLoads; ++i) {
-    const bool in = row + R::kRows * i < n;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const i16x2 v = ordered(rows.x[i][j]);
-      hi[j] = in ? __builtin_elementwise_max(hi[j], v) : hi[j];
-      lo[j] = in ? __builtin_elementwise_min(lo[j], v) : lo[j];
+    for (int i = 1; i < R::kLoads; ++i) {
+      const uint32_t v = __builtin_bit_cast(uint32_t, ordered(rows.x[i][j]));
+      hi[j] = pick<false>(hi[j], v);
+      lo[j] = pick<true>(lo[j], v);
     }
   }
-#pragma unroll
-  for (int m = R::kG; m < 64; m *= 2)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      hi[j] = __builtin_elementwise_max(hi[j], shfl_i16x2(hi[j], m));
-      lo[j] = __builtin_elementwise_min(lo[j], shfl_i16x2(lo[j], m));
-    }
+  const i16x2 most = __builtin_bit_cast(i16x2, over_rows<D, false>(hi));
+  const i16x2 least = __builtin_bit_cast(i16x2, over_rows<D, true>(lo));
   // the largest magnitude over the entries, as an ordered integer; at least kInf where one is not finite
-  int top = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) top = max(top, max((int)hi[j][e], ~(int)lo[j][e]));  // ~: a negative's magnitude
-#pragma unroll
-  for (int m = 1; m < R::kG; m *= 2) top = max(top, __shfl_xor(top, m, 64));
+  int top = max(max((int)most[0], (int)most[1]), max(~(int)least[0], ~(int)least[1]));  // ~: a negative's magnitude
+  top = wave_max(max(top, 0));
   const bool finite = top < kInf;
   // top = 1.f 2^e with 7 bits of f: 127 2^(e - 6) = 1.1111110b 2^e is at least that for f < 0x7F
   const int e = (top >> 7) - 127;
   const int unit = max(kLeastUnit, e - 6 + ((top & 0x7F) == 0x7F ? 1 : 0));
-  const float scale = __builtin_bit_cast(float, (uint32_t)(127 - unit) << 23);
-  // lanes of the first rows store the upper bounds, those of the next the lower ones
-  const bool up = row == 0;
-  uint32_t packed[2] = {0, 0};
+  const float scale = finite ? __builtin_bit_cast(float, (uint32_t)(127 - unit) << 23) : 0.0f;
+  uint32_t upper = 0, lower = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int16_t o = up ? hi[j][c] : lo[j][c];
-      const float y = value_of(o) * scale;  // exact, but for values below 2^-149, which are 1 or -1 then
-      int v = (int)(up ? ceilf(y) : floorf(y));
-      if (up && o > 0) v = max(v, 1);
-      if (!up && o < -1) v = min(v, -1);
-      packed[j >> 1] |= (uint32_t)(v & 0xFF) << (16 * (j & 1) + 8 * c);
-    }
-  if (!finite) packed[0] = packed[1] = 0;
-  if (row < 2)
-    *reinterpret_cast<uint2*>(bounds + at * (2 * D) + (up ? 0 : D) + 8 * part) = uint2{packed[0], packed[1]};
+  for (int c = 0; c < 2; ++c) {
+    // the product is exact, but for values below 2^-149, which are 1 or -1 then
+    int u = (int)ceilf(value_of(most[c]) * scale), l = (int)floorf(value_of(least[c]) * scale);
+    u = most[c] > 0 ? max(u, 1) : u;
+    l = least[c] < -1 ? min(l, -1) : l;  // (-1 is -0)
+    upper |= (uint32_t)(u & 0xFF) << (8 * c);
+    lower |= (uint32_t)(l & 0xFF) << (8 * c);
+  }
+  if (!finite) upper = lower = 0;
+  if (D == 128 || (lane & 8) == 0) {
+    int8_t* to = bounds + at * (2 * D) + 8 * part + 2 * (lane >> 4);
+    *reinterpret_cast<uint16_t*>(to) = (uint16_t)upper;
+    *reinterpret_cast<uint16_t*>(to + D) = (uint16_t)lower;
+  }
   if (lane == 0) units[at] = (int8_t)(finite ? unit : kNoUnit);
 }
 
-// One wave per (row, kv head); it works if the row is the first of its page's, and takes the rows behind
-// it that follow in the same page.
+// A workgroup looks at a.window rows (1 or 16) for the first rows of pages.  Such a row, with those behind it that
+// follow in the same page, is an item for each kv head, and the items go round the workgroups of the window
+// (gridDim.y) and their waves.
 template <int D, bool kBounds>
 __global__ __launch_bounds__(kBoundWaves * 64) void slot_append_kernel(SlotAppendArgs a) {
   using R = PageRows<D>;
-  const int lane = threadIdx.x & 63;
-  const uint32_t id = blockIdx.x * kBoundWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t nth = (int32_t)(id / (uint32_t)a.num_kv_heads), head = (int32_t)id - nth * a.num_kv_heads;
-  if (nth >= a.rows) return;
-  const int32_t row = a.first_row + nth;
-  // lane 0 the row before, lane 1 + i row + i
-  const int64_t r = (int64_t)row - 1 + lane;
-  const int64_t slot = lane <= kPage && r >= 0 && r < a.num_rows ? a.row_slot[r] : -1;
-  const int64_t slot0 = __shfl(slot, 1, 64), before = __shfl(slot, 0, 64);
-  if (slot0 < 0) return;
-  if (slot0 >= a.num_pages * kPage) {
-    if (lane == 1) atomicOr(a.error_flags, 1);
-    return;
-  }
-  const int s0 = (int)(slot0 % kPage);
-  if (s0 > 0 && before == slot0 - 1) return;
-  const uint64_t follow = __builtin_amdgcn_ballot_w64(lane > 0 && lane <= kPage - s0 && slot == slot0 + (lane - 1));
-  const int n = __builtin_ctzll(~(follow >> 1));  // rows of this page, 1 .. 16 - s0
-  const int64_t at = slot0 / kPage * a.num_kv_heads + head;
+  const int lane = threadIdx.x & 63, Hkv = a.num_kv_heads;
+  const int wave = blockIdx.y * kBoundWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = gridDim.y * kBoundWaves;
+  // lane 0 the row before the window, lane 1 + i row i of it and the 15 behind it
+  const int64_t row0 = a.first_row + (int64_t)blockIdx.x * a.window, r = row0 - 1 + lane;
+  const bool there = lane <= a.window + kPage - 1 && r >= 0 && r < a.num_rows;
+  const int64_t slot = there ? a.row_slot[r] : -1;
+  const int64_t before = __shfl_up(slot, 1, 64);
+  const bool follows = slot > 0 && slot % kPage != 0 && slot == before + 1;  // the row before it in the same page
+  const bool in_window = lane > 0 && lane <= a.window && slot >= 0;
+  const bool outside = slot >= a.num_pages * kPage;
+  if (in_window && outside && wave == 0) atomicOr(a.error_flags, 1);
+  const uint64_t chain = __builtin_amdgcn_ballot_w64(follows);
+  uint64_t firsts = __builtin_amdgcn_ballot_w64(in_window && !outside && (!follows || before < 0));
   const int part = lane % R::kG, first = lane / R::kG;
-  PageRows<D> k, v;
+  for (int turn = wave; firsts; firsts &= firsts - 1, turn -= Hkv) {  // item `turn` of this row's kv heads is this wave's
+    if (turn >= Hkv) continue;
+    const int at_lane = __builtin_ctzll(firsts);
+    const int64_t slot0 = ((int64_t)__builtin_amdgcn_readlane((int)(slot >> 32), at_lane) << 32) |
+                          (uint32_t)__builtin_amdgcn_readlane((int)slot, at_lane);
+    const int s0 = (int)(slot0 % kPage);
+    const int n = __builtin_ctzll(~(chain >> at_lane >> 1)) + 1;  // rows of this page, 1 .. 16 - s0
+    const int64_t row = row0 - 1 + at_lane;
+    for (; turn < Hkv; turn += waves) {
+      const int64_t at = slot0 / kPage * Hkv + turn;
+      PageRows<D> k, v;
 #pragma unroll
-  for (int i = 0; i < R::kLoads; ++i) {
-    const int s = first + R::kRows * i;
-    k.x[i] = v.x[i] = zero_u32x4();
-    if (s >= s0 && s < s0 + n) {
-      const int64_t src = (((int64_t)row + s - s0) * a.num_kv_heads + head) * D + 8 * part;
-      k.x[i] = load_u32x4(a.k_new + src);
-      v.x[i] = load_u32x4(a.v_new + src);
-    } else if (kBounds && s < s0) {
-      k.x[i] = load_u32x4(a.k_pool + (at * kPage + s) * D + 8 * part);
+      for (int i = 0; i < R::kLoads; ++i) {
+        // slots past the new rows: the last of them again, for the bounds
+        const int s = first + R::kRows * i, from = max(0, min(s - s0, n - 1));
+        const int64_t src = ((row + from) * Hkv + turn) * D + 8 * part;
+        if (kBounds) {
+          k.x[i] = load_u32x4(s < s0 ? a.k_pool + (at * kPage + s) * D + 8 * part : a.k_new + src);
+          v.x[i] = load_u32x4(a.v_new + src);
+        } else if (s >= s0 && s < s0 + n) {
+          k.x[i] = load_u32x4(a.k_new + src);
+          v.x[i] = load_u32x4(a.v_new + src);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < R::kLoads; ++i) {
+        const int s = first + R::kRows * i;
+        if (s >= s0 && s < s0 + n) {
+          store_u32x4(a.k_pool + (at * kPage + s) * D + 8 * part, k.x[i]);
+          store_u32x4(a.v_pool + (at * kPage + s) * D + 8 * part, v.x[i]);
+        }
+      }
+      if constexpr (kBounds) put_bounds<D>(k, a.bounds, a.units, at);
     }
   }
-#pragma unroll
-  for (int i = 0; i < R::kLoads; ++i) {
-    const int s = first + R::kRows * i;
-    if (s >= s0 && s < s0 + n) {
-      store_u32x4(a.k_pool + (at * kPage + s) * D + 8 * part, k.x[i]);
-      store_u32x4(a.v_pool + (at * kPage + s) * D + 8 * part, v.x[i]);
-    }
-  }
-  if constexpr (kBounds) put_bounds<D>(k, s0 + n, a.bounds, a.units, at);
 }
 
 // One wave per (task, kBoundPages pages, kv head): all of them in flight at once.
@@ -196,23 +226,29 @@ __global__ __launch_bounds__(kBoundWaves * 64) void key_bounds_kernel(KeyBoundsA
   for (int i = 0; i < kBoundPages; ++i)
 #pragma unroll
     for (int j = 0; j < R::kLoads; ++j) {
-      k[i].x[j] = zero_u32x4();
-      if (at[i] >= 0 && lane / R::kG + R::kRows * j < n[i])
-        k[i].x[j] = load_u32x4(a.k_pool + at[i] * kPage * D + 8 * (lane + 64 * j));
+      const int s = max(0, min(lane / R::kG + R::kRows * j, n[i] - 1));
+      if (at[i] >= 0)
+        k[i].x[j] = __builtin_nontemporal_load(
+            reinterpret_cast<const u32x4*>(a.k_pool + (at[i] * kPage + s) * D + 8 * (lane % R::kG)));
     }
 #pragma unroll
   for (int i = 0; i < kBoundPages; ++i)
-    if (at[i] >= 0) put_bounds<D>(k[i], n[i], a.bounds, a.units, at[i]);
+    if (at[i] >= 0) put_bounds<D>(k[i], a.bounds, a.units, at[i]);
 }
 
 template <int D>
 hipError_t append_slots(const SlotAppendArgs& args, hipStream_t stream) {
   SlotAppendArgs a = args;
+  // Few rows: a workgroup for 4 kv heads of each, so that the call ends soon.  More than the device holds waves:
+  // one for 16 rows, since 15 of 16 rows of an observation are not the first of a page, and a wave that only finds
+  // that out costs a third of one that works (35,144 rows of 4 heads: a wave a row and head 47 us, a wave a row 35).
+  a.window = (int64_t)a.num_rows * a.num_kv_heads > kAppendWaves ? kPage : 1;
+  const uint32_t parts = a.window > 1 ? 1 : (uint32_t)((a.num_kv_heads + kBoundWaves - 1) / kBoundWaves);
   // a launch holds fewer than 2^32 threads
-  const int32_t most = std::max(1, (1 << 25) / a.num_kv_heads);
-  for (a.first_row = 0; a.first_row < a.num_rows; a.first_row += a.rows) {
-    a.rows = std::min(most, a.num_rows - a.first_row);
-    const uint32_t blocks = (uint32_t)(((int64_t)a.rows * a.num_kv_heads + kBoundWaves - 1) / kBoundWaves);
+  const int32_t most = (int32_t)((1 << 23) / parts) * a.window;
+  for (int64_t row = 0; row < a.num_rows; row += most) {
+    a.first_row = (int32_t)row;
+    const dim3 blocks((uint32_t)((std::min<int64_t>(most, a.num_rows - row) + a.window - 1) / a.window), parts);
     if (a.bounds)
       hipLaunchKernelGGL((slot_append_kernel<D, true>), dim3(blocks), dim3(kBoundWaves * 64), 0, stream, a);
     else

@@ -9,9 +9,11 @@
 // Both sums only grow, so a refusal holds for every later task that needs one more, and what is
 // granted is one run from the top: the result does not depend on the order of threads.
 //
-// One workgroup scans the tasks, 1,024 a round, and then writes pages and rows element by element: each
+// One workgroup scans the tasks, 2,048 a round, and then writes pages and rows element by element: each
 // finds its task by bisection of the sums in LDS, so one long task costs no more than many short ones.
 // Above kRowsHere rows a second kernel writes the rows from the results of the first.
+#include <type_traits>
+
 #include "kernels.h"
 #include "tide_device.h"
 
@@ -19,6 +21,8 @@ namespace tide {
 namespace kern {
 
 constexpr int kMapThreads = 1024;
+constexpr int kMapTasks = 2048;  // of a round
+constexpr int kMany = 4;  // pages or rows of a thread whose bisections and loads are in flight together
 constexpr int kRowThreads = 256;
 constexpr int kRowTasks = 4096;  // tasks whose row starts the second kernel keeps in LDS
 
@@ -58,6 +62,22 @@ __device__ __forceinline__ int last_at_most(const T* first, int n, T j) {
   return lo;
 }
 
+// The same for several values, whose reads are in flight together.
+template <int kAtOnce>
+__device__ __forceinline__ void last_at_most(const uint32_t* first, int n, const uint32_t (&j)[kAtOnce], int (&at)[kAtOnce]) {
+#pragma unroll
+  for (int u = 0; u < kAtOnce; ++u) at[u] = 0;
+  while (n > 1) {
+    const int half = n >> 1;
+    uint32_t x[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) x[u] = first[at[u] + half];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) at[u] += x[u] <= j[u] ? half : 0;
+    n -= half;
+  }
+}
+
 __device__ __forceinline__ int32_t pages_of(int32_t len) { return (int32_t)(((int64_t)len + kPage - 1) / kPage); }
 
 __device__ __forceinline__ void put_row(const PageMapArgs& a, int64_t r, int32_t task, int32_t pos, int64_t slot) {
@@ -68,93 +88,179 @@ __device__ __forceinline__ void put_row(const PageMapArgs& a, int64_t r, int32_t
 
 __global__ __launch_bounds__(kMapThreads) void page_map_kernel(PageMapArgs a) {
   __shared__ uint32_t tmp[4][kMapThreads / 64];
-  __shared__ uint32_t first_page[kMapThreads], first_row[kMapThreads];
-  __shared__ int32_t len_of[kMapThreads], want_of[kMapThreads];  // want: that of the call, or the length where refused
+  __shared__ uint32_t first_page[kMapTasks], first_row[kMapTasks];
+  __shared__ int32_t len_of[kMapTasks], want_of[kMapTasks];  // want: that of the call, or the length where refused
   __shared__ uint32_t used;
   const int tid = threadIdx.x;
   const uint32_t count = (uint32_t)min(max(*a.free_count, 0), a.capacity);
   const int64_t most = (int64_t)a.bt_stride * kPage;
   if (tid == 0) used = 0;
 
-  auto load = [&](int b, int32_t* len, int32_t* want) {  // a task whose lengths are no lengths stays as it is
-    *len = *want = 0;
-    if (b >= a.num_tasks) return;
-    *len = a.lens[b];
-    *want = a.want[b];
-    if (*len < 0 || *len > most || *want < 0 || *want > most) *want = *len;
+  // a thread's two neighbouring tasks of a round; one whose lengths are no lengths stays as it is
+  int32_t len[2], want[2];
+  auto load = [&](int b) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      len[c] = want[c] = 0;
+      if (b + c >= a.num_tasks) continue;
+      len[c] = a.lens[b + c];
+      want[c] = a.want[b + c];
+      if (len[c] < 0 || len[c] > most || want[c] < 0 || want[c] > most) want[c] = len[c];
+    }
+  };
+  // sums of x over the tasks before each of a thread's two
+  auto sums_before = [&](const uint32_t (&x)[2], uint32_t* scratch, uint32_t (&before)[2], uint32_t* all) {
+    const uint32_t both = sat_add(x[0], x[1]), upto = map_scan(both, scratch, all);
+    before[0] = upto - both;  // (callers whose sums may be cut off use the sums up to a task instead)
+    before[1] = sat_add(before[0], x[0]);
+    return upto;
+  };
+
+  // f(how many elements of `all` a thread takes at once)
+  auto by_width = [](uint32_t all, auto&& f) {
+    if (all > kMapThreads) f(std::integral_constant<int, kMany>());
+    else f(std::integral_constant<int, 1>());
   };
 
   // pages that go back, on top of the stack
+  const bool one_round = a.num_tasks <= kMapTasks;
   uint32_t back = 0;
-  for (int t0 = 0; t0 < a.num_tasks; t0 += kMapThreads) {
-    int32_t len, want;
-    load(t0 + tid, &len, &want);
-    const uint32_t n = want < len ? (uint32_t)(pages_of(len) - pages_of(want)) : 0u;
-    uint32_t all;
-    const uint32_t in = map_scan(n, tmp[0], &all);
-    first_page[tid] = in - n;  // (a table has fewer than 2^31 entries, so these sums are exact)
-    len_of[tid] = want;
-    __syncthreads();
-    const int tasks = min(kMapThreads, a.num_tasks - t0);
-    for (uint32_t j = tid; j < all; j += kMapThreads) {
-      const int i = last_at_most(first_page, tasks, j);
-      const uint32_t at = sat_add(sat_add(count, back), j);
-      if (at < (uint32_t)a.capacity)
-        a.free_pages[at] = a.block_table[(int64_t)(t0 + i) * a.bt_stride + pages_of(len_of[i]) + (int32_t)(j - first_page[i])];
+  for (int t0 = 0; t0 < a.num_tasks; t0 += kMapTasks) {
+    load(t0 + 2 * tid);
+    uint32_t n[2], before[2], all;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) n[c] = want[c] < len[c] ? (uint32_t)(pages_of(len[c]) - pages_of(want[c])) : 0u;
+    sums_before(n, tmp[0], before, &all);  // (a table has fewer than 2^31 entries, so these sums are exact)
+    if (all > 0) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) first_page[2 * tid + c] = before[c], len_of[2 * tid + c] = want[c];
+      __syncthreads();
+      const int tasks = min(kMapTasks, a.num_tasks - t0);
+      auto give_back = [&](auto at_once) {
+        constexpr int kAtOnce = decltype(at_once)::value;
+        for (uint32_t j0 = tid; j0 < all; j0 += kAtOnce * kMapThreads) {
+          uint32_t j[kAtOnce];
+          int i[kAtOnce];
+          int32_t page[kAtOnce];
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) j[u] = min(j0 + u * kMapThreads, all - 1);
+          last_at_most(first_page, tasks, j, i);
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u)
+            page[u] = a.block_table[(int64_t)(t0 + i[u]) * a.bt_stride + pages_of(len_of[i[u]]) +
+                                    (int32_t)(j[u] - first_page[i[u]])];
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) {
+            const uint32_t at = sat_add(sat_add(count, back), j[u]);
+            if (j0 + u * kMapThreads < all && at < (uint32_t)a.capacity) a.free_pages[at] = page[u];
+          }
+        }
+      };
+      by_width(all, give_back);
+      back = sat_add(back, all);
     }
-    back = sat_add(back, all);
     __syncthreads();
   }
   const uint32_t there = min(sat_add(count, back), (uint32_t)a.capacity);
 
   // rows and pages of the tasks that grow
   uint32_t asked = 0, rows = 0, pages = 0;
-  for (int t0 = 0; t0 < a.num_tasks; t0 += kMapThreads) {
-    const int b = t0 + tid, tasks = min(kMapThreads, a.num_tasks - t0);
-    int32_t len, want;
-    load(b, &len, &want);
-    uint32_t e = want > len ? (uint32_t)(want - len) : 0u, all_e, all_r, all_p;
-    const uint32_t end_e = sat_add(asked, map_scan(e, tmp[1], &all_e));
-    if (end_e > (uint32_t)a.num_rows) {  // no rows left: refused
-      if (e) want = len;
-      e = 0;
+  for (int t0 = 0; t0 < a.num_tasks; t0 += kMapTasks) {
+    const int b = t0 + 2 * tid, tasks = min(kMapTasks, a.num_tasks - t0);
+    if (!one_round) load(b);
+    uint32_t e[2], p[2], in_r[2], in_p[2], all_e, all_r, all_p;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) e[c] = want[c] > len[c] ? (uint32_t)(want[c] - len[c]) : 0u;
+    // (sums may be cut off here: the one up to the thread's first task is taken from those before the thread)
+    const uint32_t both = sat_add(e[0], e[1]);
+    uint32_t upto = map_scan(both, tmp[1], &all_e);
+    const uint32_t upto_prev = (uint32_t)__shfl_up((int)upto, 1, 64);
+    uint32_t start = (tid & 63) ? upto_prev : 0;
+    if ((tid & 63) == 0) {
+#pragma unroll
+      for (int w = 0; w < kMapThreads / 64; ++w) start = w < (tid >> 6) ? sat_add(start, tmp[1][w]) : start;
     }
-    const uint32_t p = e ? (uint32_t)(pages_of(want) - pages_of(len)) : 0u;
-    const uint32_t in_r = map_scan(e, tmp[2], &all_r), in_p = map_scan(p, tmp[3], &all_p);
-    const uint32_t end_p = sat_add(pages, in_p);
-    const bool short_of = p > 0 && end_p > there;
-    if (p > 0 && !short_of) atomicMax(&used, end_p);
-    first_row[tid] = in_r - e;
-    first_page[tid] = in_p - p;
-    len_of[tid] = len;
-    want_of[tid] = short_of ? len : want;
-    if (b < a.num_tasks) {
-      a.row_start[b] = (int32_t)(rows + in_r - e);
-      a.lens_out[b] = short_of ? len : want;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      start = sat_add(start, e[c]);
+      if (sat_add(asked, start) > (uint32_t)a.num_rows) {  // no rows left: refused
+        if (e[c]) want[c] = len[c];
+        e[c] = 0;
+      }
+      p[c] = e[c] ? (uint32_t)(pages_of(want[c]) - pages_of(len[c])) : 0u;
+    }
+    sums_before(e, tmp[2], in_r, &all_r);  // (at most num_rows)
+    sums_before(p, tmp[3], in_p, &all_p);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint32_t end_p = sat_add(pages, in_p[c] + p[c]);
+      const bool short_of = p[c] > 0 && end_p > there;
+      if (p[c] > 0 && !short_of) atomicMax(&used, end_p);
+      const int32_t to = short_of ? len[c] : want[c];
+      first_row[2 * tid + c] = in_r[c];
+      first_page[2 * tid + c] = in_p[c];
+      len_of[2 * tid + c] = len[c];
+      want_of[2 * tid + c] = to;
+      if (b + c < a.num_tasks) {
+        a.row_start[b + c] = (int32_t)(rows + in_r[c]);
+        a.lens_out[b + c] = to;
+      }
     }
     __syncthreads();
     const uint32_t granted = min(all_p, there - min(there, pages));  // pages this round may take, some refused
-    for (uint32_t j = tid; j < granted; j += kMapThreads) {
-      const int i = last_at_most(first_page, tasks, j);
-      const int32_t lp = pages_of(len_of[i]) + (int32_t)(j - first_page[i]);
-      if (lp < pages_of(want_of[i]))
-        a.block_table[(int64_t)(t0 + i) * a.bt_stride + lp] = a.free_pages[there - 1 - pages - j];
-    }
-    if (!a.rows_apart)
-      for (uint32_t r = tid; r < all_r; r += kMapThreads) {
-        const int i = last_at_most(first_row, tasks, r);
-        const int32_t l = len_of[i], pos = l + (int32_t)(r - first_row[i]);
-        if (pos >= want_of[i]) {
-          put_row(a, rows + r, -1, -1, -1);
-          continue;
+    auto take = [&](auto at_once) {
+      constexpr int kAtOnce = decltype(at_once)::value;
+      for (uint32_t j0 = tid; j0 < granted; j0 += kAtOnce * kMapThreads) {
+        uint32_t j[kAtOnce];
+        int i[kAtOnce];
+        int32_t page[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          j[u] = min(j0 + u * kMapThreads, granted - 1);
+          page[u] = a.free_pages[there - 1 - pages - j[u]];
         }
-        const int32_t lp = pos / kPage, own = pages_of(l);  // pages before `own` are the table's, the others new
-        const int32_t page = lp < own ? a.block_table[(int64_t)(t0 + i) * a.bt_stride + lp]
-                                      : a.free_pages[there - 1 - pages - first_page[i] - (uint32_t)(lp - own)];
-        put_row(a, rows + r, t0 + i, pos, page < 0 ? -1 : (int64_t)page * kPage + pos % kPage);
+        last_at_most(first_page, tasks, j, i);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int32_t lp = pages_of(len_of[i[u]]) + (int32_t)(j[u] - first_page[i[u]]);
+          if (j0 + u * kMapThreads < granted && lp < pages_of(want_of[i[u]]))
+            a.block_table[(int64_t)(t0 + i[u]) * a.bt_stride + lp] = page[u];
+        }
       }
+    };
+    by_width(granted, take);
+    auto write_rows = [&](auto at_once) {
+      constexpr int kAtOnce = decltype(at_once)::value;
+      for (uint32_t r0 = tid; r0 < all_r; r0 += kAtOnce * kMapThreads) {
+        uint32_t r[kAtOnce];
+        int i[kAtOnce];
+        int32_t pos[kAtOnce], page[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) r[u] = min(r0 + u * kMapThreads, all_r - 1);
+        last_at_most(first_row, tasks, r, i);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int32_t l = len_of[i[u]];
+          pos[u] = l + (int32_t)(r[u] - first_row[i[u]]);
+          // pages before `own` are the table's, the others new
+          const int32_t lp = pos[u] / kPage, own = pages_of(l);
+          page[u] = -1;
+          if (pos[u] < want_of[i[u]])
+            page[u] = lp < own ? a.block_table[(int64_t)(t0 + i[u]) * a.bt_stride + lp]
+                               : a.free_pages[there - 1 - pages - first_page[i[u]] - (uint32_t)(lp - own)];
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          if (r0 + u * kMapThreads >= all_r) continue;
+          const bool ok = pos[u] < want_of[i[u]];
+          put_row(a, rows + r[u], ok ? t0 + i[u] : -1, ok ? pos[u] : -1,
+                  page[u] < 0 ? -1 : (int64_t)page[u] * kPage + pos[u] % kPage);
+        }
+      }
+    };
+    if (!a.rows_apart) by_width(all_r, write_rows);
     asked = sat_add(asked, all_e);
-    rows += all_r;  // (at most num_rows)
+    rows += all_r;
     pages = sat_add(pages, all_p);
     __syncthreads();
   }

@@ -541,9 +541,10 @@ struct SlotAppendArgs {
   int64_t num_pages;
   int32_t num_kv_heads;
   int32_t num_rows;
-  int32_t first_row, rows;  // of the launch
-  int8_t* bounds;           // [num_pages][Hkv][2][d], may be null
-  int8_t* units;            // [num_pages][Hkv]
+  int32_t first_row;  // of the launch
+  int32_t window;     // rows of a workgroup
+  int8_t* bounds;     // [num_pages][Hkv][2][d], may be null
+  int8_t* units;      // [num_pages][Hkv]
   int32_t* error_flags;
 };
 
