@@ -24,7 +24,7 @@ HIP_SOURCES = ["tide_api.hip", "attn_extend.hip", "attn_extend_append.hip", "att
                "attn_decode_stream.hip",
                "kv_append.hip", "cache_api.hip", "kv4_store.hip", "kv4_decode.hip", "attn_mass.hip",
                "kv_evict.hip", "rows_api.hip", "page_map.hip", "key_bounds.hip", "block_select.hip",
-               "sparse_attn.hip"]
+               "sparse_attn.hip", "sparse_shared.hip"]
 CXX_SOURCES = ["plan.cpp", "ctb.cpp"]
 ARCH = "gfx950"
 

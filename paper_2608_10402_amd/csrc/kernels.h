@@ -40,6 +40,8 @@ hipError_t launch_slot_append(const SlotAppendArgs& a, int head_dim, hipStream_t
 hipError_t launch_key_bounds(const KeyBoundsArgs& a, int head_dim, int32_t num_tasks, hipStream_t stream);
 hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, hipStream_t stream);
 hipError_t launch_sparse(const SparseArgs& a, int head_dim, bool shared, hipStream_t stream);
+// The same for rows of which several belong to one task.
+hipError_t launch_sparse_shared(const SparseArgs& a, int head_dim, hipStream_t stream);
 // Query rows that a wave of the score kernel takes at once.
 int select_tile_rows(int32_t group, bool chunk);
 

@@ -79,6 +79,19 @@ size_t sparse_bytes(int32_t num_rows, int32_t budget, const tide_dims& dims, siz
   return *ml_off + rows * 16;
 }
 
+// Rows that a workgroup takes at once: 1 where rows have tasks of their own or are too few to fill the device, and
+// where their lists or contexts are longer than a workgroup can mark.
+void shared_rows(int32_t num_rows, int32_t num_tasks, int32_t budget, int32_t bt_stride, const tide_dims& dims,
+                 int32_t splits, int32_t* rows, int32_t* shift) {
+  const int32_t group = dims.num_q_heads / dims.num_kv_heads;
+  *shift = 0;
+  while ((1 << *shift) < group) ++*shift;
+  *rows = 1;
+  if (num_rows <= num_tasks || splits > 1) return;
+  if (bt_stride > (dims.head_dim == 128 ? kSharedBlocks<128> : kSharedBlocks<64>)) return;
+  *rows = std::max(1, std::min({kSharedRows, 32 >> *shift, kSharedEntries / budget}));
+}
+
 }  // namespace
 }  // namespace tide
 
@@ -328,12 +341,14 @@ TIDE_API int tide_sparse_attn(const void* q, const void* k_pool, const void* v_p
     a.error_flags = at_mut<int32_t>(workspace, 0);
     // rows of one task share pages; a row of its own streams them
     const bool shared = num_rows > num_tasks;
-    const int64_t most = std::max<int64_t>(1, kSparseLaunch / ((int64_t)a.num_kv_heads * a.splits));
+    shared_rows(num_rows, num_tasks, budget, bt_stride, *dims, a.splits, &a.rows_at_once, &a.padded_shift);
+    int64_t most = std::max<int64_t>(1, kSparseLaunch / ((int64_t)a.num_kv_heads * a.splits));
+    most -= a.rows_at_once > 1 ? most % a.rows_at_once : 0;
     hipError_t err = hipSuccess;
     for (int64_t first = 0; first < num_rows && err == hipSuccess; first += most) {
       a.first_row = (int32_t)first;
       a.rows = (int32_t)std::min<int64_t>(most, num_rows - first);
-      err = launch_sparse(a, dims->head_dim, shared, s);
+      err = a.rows_at_once > 1 ? launch_sparse_shared(a, dims->head_dim, s) : launch_sparse(a, dims->head_dim, shared, s);
     }
     Staged none;
     return finish(err, none, workspace, s);

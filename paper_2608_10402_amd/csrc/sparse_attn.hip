@@ -152,18 +152,18 @@ void sparse_attn_kernel(SparseArgs a) {
 #pragma unroll
       for (int c = 0; c < kC; ++c) s[t] = mfma16(as_bf16x8(kk[t][c]), qf[c], s[t]);
     }
-    float mt = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
+    if (st.n0 + st.n1 < 2 * kPage) {  // keys past the position
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = 4 * grp + e < (t ? st.n1 : st.n0) ? s[t][e] * a.scale_log2 : -INFINITY;
-        s[t][e] = x;
-        mt = fmaxf(mt, x);
+        s[0][e] = 4 * grp + e < st.n0 ? s[0][e] : -INFINITY;
+        s[1][e] = 4 * grp + e < st.n1 ? s[1][e] : -INFINITY;
       }
-    mt = fmaxf(mt, xor_shfl(mt, 16));
-    mt = fmaxf(mt, xor_shfl(mt, 32));
-    if (__any(mt > m_ref + kRescaleSlack)) {
+    }
+    float mt = a.scale_log2 * fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                                    fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    if (__any(mt > m_ref + kRescaleSlack)) {  // only then is the column's maximum worked out
+      mt = fmaxf(mt, xor_shfl(mt, 16));
+      mt = fmaxf(mt, xor_shfl(mt, 32));
       const float m_new = fmaxf(m_ref, mt);
       const float alpha = fast_exp2(m_ref - m_new);
       l_part *= alpha;
@@ -177,8 +177,8 @@ void sparse_attn_kernel(SparseArgs a) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float p0 = fast_exp2(s[t][2 * e] - m_ref);
-        const float p1 = fast_exp2(s[t][2 * e + 1] - m_ref);
+        const float p0 = fast_exp2(fmaf(s[t][2 * e], a.scale_log2, -m_ref));
+        const float p1 = fast_exp2(fmaf(s[t][2 * e + 1], a.scale_log2, -m_ref));
         // weights go to the P V product in bf16; the sum that divides it is of the rounded ones
         wp[2 * t + e] = pack_bf16x2(p0, p1);
         l_part = add_bf16x2(wp[2 * t + e], l_part);

@@ -1,0 +1,436 @@
+// Attention of rows over block lists (sparse_attn.hip), several rows of one task at a time.
+//
+// Neighbouring rows of a task list mostly the same blocks, and a step of one row fills G of the 16 columns of an
+// MFMA.  One workgroup here takes up to 8 rows of a kv head, 32 / P of them, where P is the least power of two of
+// at least G: it marks which row lists which block (a byte a block in LDS), packs the marked blocks, and walks
+// them as the one-row kernel walks a list, with the rows' heads as the columns of one or two products that share
+// every K and V operand.  A column takes part where its row's mark is set and the key is not past its position.
+// Its traffic is the union of the lists, not their sum: 1,761 rows of 128 blocks each over 8 contexts of 32k-98k
+// (64 / 8 heads, d = 128) take 675 us by single rows, which is what the L1s deliver (16 KB a step of 32 keys).
+//
+// What rows do not share must not reach them: a weight of zero times a V that is not finite is NaN.  The outputs
+// of rows taken together are looked at, and rows with one that is not finite are taken again, one by one; so are
+// rows that list a block twice, which a mark does not count.
+#include <algorithm>
+
+#include "attn_decode.h"
+
+namespace tide {
+namespace kern {
+
+constexpr float kNoKeysYet = -3.0e38f;  // as kNoKeys of sparse_attn.hip
+constexpr int kSharedWaves = 4, kSharedThreads = kSharedWaves * 64;
+
+// The same number, which the compiler cannot see through: offsets made from it stay where they are used.  Kept from
+// one turn of the loop over tasks to the next they cost more registers than there are.
+__device__ __forceinline__ int unknown(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// An entry of the packed list: the block in the upper 24 bits, the rows that list it in the lower 8.
+struct SharedStep {
+  int n0, n1;              // 1 where the step has the entry
+  uint32_t what0, what1;
+};
+
+template <int D, int kTiles>
+__global__ __launch_bounds__(kSharedThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void sparse_shared_kernel(SparseArgs a) {
+  using KL = KLds<D>;
+  using VL = VLds<D>;
+  constexpr int kC = D / 32, kT = D / 16, kWaves = kSharedWaves;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int Hkv = a.num_kv_heads, G = a.group, R = a.rows_at_once, shift = a.padded_shift;
+  const int nth = blockIdx.x / Hkv, head = blockIdx.x - nth * Hkv;
+  const int64_t row0 = (int64_t)a.first_row + (int64_t)nth * R;
+  // K pages of the two steps in flight; marks before them, outputs after them
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[kWaves * 2 * KL::kPageBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[kWaves * 2 * KL::kPageBytes];
+  __shared__ int32_t list_page[kSharedEntries];
+  __shared__ uint32_t list_what[kSharedEntries];
+  __shared__ f32x4 stats[kWaves][16 * kTiles];
+  __shared__ uint32_t sums[kWaves], flags;  // flags: rows that have to be taken again
+  static_assert(sizeof(k_lds0) >= kSharedBlocks<D>, "a mark a block");
+  uint8_t* const ka = k_lds0 + wave * 2 * KL::kPageBytes;
+  uint8_t* const kb = k_lds1 + wave * 2 * KL::kPageBytes;
+  uint32_t* const marks = reinterpret_cast<uint32_t*>(k_lds0);
+  const uint8_t* kpool = reinterpret_cast<const uint8_t*>(a.k_pool);
+  const uint8_t* vpool = reinterpret_cast<const uint8_t*>(a.v_pool);
+  constexpr int64_t kBlk = (int64_t)kPage * D * 2;
+
+  // lane r: row r
+  int my_task = -1, my_pos = -1;
+  if (lane < R && (int64_t)nth * R + lane < a.rows) {
+    my_task = a.row_task[row0 + lane];
+    my_pos = a.row_pos[row0 + lane];
+    if (!live_row(my_task, my_pos, a.num_tasks, (int64_t)a.bt_stride * kPage)) my_task = -1;
+  }
+  uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(my_task >= 0), solo = 0;
+  bool flag_error = false;
+  while (left) {
+    const int r0 = __builtin_ctz(left), task = __builtin_amdgcn_readlane(my_task, r0);
+    const uint32_t same = (uint32_t)__builtin_amdgcn_ballot_w64(my_task == task) & left & ~solo;
+    const uint32_t subset = (solo >> r0) & 1 ? 1u << r0 : same;
+    const bool alone = (subset & (subset - 1)) == 0;
+    const int32_t* table = a.block_table + (int64_t)task * a.bt_stride;
+    int least = INT32_MAX, last = -1;  // positions
+    for (uint32_t rows = subset; rows; rows &= rows - 1) {
+      const int pos = __builtin_amdgcn_readlane(my_pos, __builtin_ctz(rows));
+      least = min(least, pos);
+      last = max(last, pos);
+    }
+    auto page_of = [&](int b) {
+      const int32_t page = table[b];
+      const bool ok = page >= 0 && page < a.num_pages;
+      flag_error |= !ok;
+      return ok ? page : -1;
+    };
+
+    // ---- the packed list ----
+    int entries;
+    const int me = unknown(tid);
+    if (me == 0) flags = 0;
+    if (alone) {
+      entries = a.budget;
+      const int32_t* list = a.sel + ((row0 + r0) * Hkv + head) * a.budget;
+      for (int i = me; i < entries; i += kSharedThreads) {
+        const int32_t b = list[i];
+        const bool in = b >= 0 && b <= last / kPage;
+        list_page[i] = in ? page_of(b) : -1;
+        list_what[i] = (uint32_t)(in ? b : 0) << 8 | subset;
+      }
+    } else {
+      const int words = (last / kPage + 4) / 4;
+      for (int i = me; i < words; i += kSharedThreads) marks[i] = 0;
+      __syncthreads();
+      for (int r = r0; r < R; ++r) {
+        if (!((subset >> r) & 1)) continue;
+        const int blocks = __builtin_amdgcn_readlane(my_pos, r) / kPage + 1;
+        const int32_t* list = a.sel + ((row0 + r) * Hkv + head) * a.budget;
+        for (int i = me; i < a.budget; i += kSharedThreads) {
+          const int32_t b = list[i];
+          if (b < 0 || b >= blocks) continue;
+          const uint32_t bit = 1u << (8 * (b & 3) + r);
+          if (atomicOr(&marks[b >> 2], bit) & bit) flags = 1u;  // (any thread that finds it writes the same)
+        }
+      }
+      __syncthreads();
+      const bool twice = flags != 0;
+      __syncthreads();
+      if (twice) {
+        solo |= subset;
+        continue;
+      }
+      // a thread packs `per` words
+      const int per = (words + kSharedThreads - 1) / kSharedThreads, w0 = min(words, me * per), w1 = min(words, w0 + per);
+      uint32_t count = 0;
+      for (int w = w0; w < w1; ++w) {
+        const uint32_t m = marks[w];
+        count += ((m & 0xFF) != 0) + ((m & 0xFF00) != 0) + ((m & 0xFF0000) != 0) + ((m >> 24) != 0);
+      }
+      // sums over the lanes before this one, bit by bit (a shuffle's lane addresses would be kept in registers)
+      uint32_t to = 0, all = 0;
+      for (int k = 0; (4 * per) >> k; ++k) {
+        const uint64_t who = __builtin_amdgcn_ballot_w64((count >> k) & 1);
+        to += __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0)) << k;
+        all += (uint32_t)__popcll(who) << k;
+      }
+      if (lane == 0) sums[wave] = all;
+      __syncthreads();
+      entries = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        to += w < wave ? sums[w] : 0u;
+        entries += (int)sums[w];
+      }
+      entries = __builtin_amdgcn_readfirstlane(entries);
+      for (int w = w0; w < w1; ++w) {
+        const uint32_t m = marks[w];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t rows = (m >> (8 * i)) & 0xFF;
+          if (rows) {
+            list_page[to] = page_of(4 * w + i);
+            list_what[to++] = (uint32_t)(4 * w + i) << 8 | rows;
+          }
+        }
+      }
+    }
+    __syncthreads();
+
+    // ---- its attention ----
+    const int l0 = unknown(lane);
+    uint32_t k_src[KL::kDma];
+#pragma unroll
+    for (int i = 0; i < KL::kDma; ++i) k_src[i] = KL::src_offset(i, l0);
+    const uint32_t k_rd_even = KL::lds_offset(l0 & 15, l0 >> 4), k_rd_odd = KL::lds_offset(l0 & 15, 4 + (l0 >> 4));
+    const uint32_t v_off = (uint32_t)(16 * l0);
+    constexpr int kRpl = 1024 / (2 * D);
+    uint32_t v_wr[DecodeRegs<D>::kLoads];
+#pragma unroll
+    for (int i = 0; i < DecodeRegs<D>::kLoads; ++i)
+      v_wr[i] = VL::offset(i * kRpl + l0 / VL::kNG, l0 % VL::kNG);
+    const int vr = 4 * (l0 >> 4) + ((l0 & 15) >> 2);
+    // (of piece t: v_rd ^ 32 t, since a row's swizzle is an exclusive or of the same bits; registers are scarce here)
+    const uint32_t v_rd = (uint32_t)(vr * 2 * D + 32 * VL::vsw(vr) + 8 * (l0 & 3));
+    const int pairs = (entries + 1) / 2;
+    int next_pair = wave;
+    int32_t page = 0;
+    uint32_t what = 0;
+    uint64_t open = 0;
+    auto fetch = [&]() {
+      while (open == 0 && next_pair < pairs) {
+        const int at = 2 * (next_pair + kWaves * (lane >> 1)) + (lane & 1);
+        next_pair += 32 * kWaves;
+        page = at < entries ? list_page[at] : -1;
+        what = at < entries ? list_what[at] : 0;
+        open = __builtin_amdgcn_ballot_w64(page >= 0);
+      }
+    };
+    auto issue = [&](DecodeRegs<D>& r, uint8_t* kbuf) {
+      fetch();
+      int64_t b0 = 0, b1 = 0;
+      SharedStep s = {0, 0, 0, 0};
+      if (open) {
+        const int i = __builtin_ctzll(open);
+        open &= open - 1;
+        s.n0 = 1;
+        s.what0 = (uint32_t)__builtin_amdgcn_readlane((int)what, i);
+        b0 = ((int64_t)__builtin_amdgcn_readlane(page, i) * Hkv + head) * kBlk;
+      }
+      if (open) {
+        const int i = __builtin_ctzll(open);
+        open &= open - 1;
+        s.n1 = 1;
+        s.what1 = (uint32_t)__builtin_amdgcn_readlane((int)what, i);
+        b1 = ((int64_t)__builtin_amdgcn_readlane(page, i) * Hkv + head) * kBlk;
+      }
+      const int z0 = s.n0 ? (int)kBlk : 0, z1 = s.n1 ? (int)kBlk : 0;
+      load_step<D, kSharedPolicy>(r, kbuf, block_rsrc(kpool + b0, z0), block_rsrc(kpool + b1, z1),
+                                  block_rsrc(vpool + b0, z0), block_rsrc(vpool + b1, z1), k_src, v_off);
+      return s;
+    };
+
+    // column `col` of product t: row and head, its bit, its position
+    uint32_t bit[kTiles], tile_rows[kTiles];
+    int pos_of[kTiles];
+    bf16x8 qf[kTiles][kC];
+    f32x4 o[kTiles][kT];
+    float m_ref[kTiles], l_part[kTiles], l_exact[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const int r = (16 * t + col) >> shift, h = (16 * t + col) & ((1 << shift) - 1);
+      const bool on = h < G && r < R && (subset >> r) & 1;
+      bit[t] = on ? 1u << r : 0;
+      pos_of[t] = __shfl(my_pos, r & 63, 64);
+      const int first = (16 * t) >> shift, end = (16 * t + 15) >> shift;
+      tile_rows[t] = subset & ((2u << min(end, 30)) - (1u << min(first, 30)));
+      const int64_t at = ((row0 + (on ? r : r0)) * a.num_q_heads + head * G + (on ? h : 0)) * D;
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        const u32x4 x = load_u32x4(a.q + at + 32 * c + 8 * grp);
+        qf[t][c] = as_bf16x8(on ? x : zero_u32x4());
+      }
+#pragma unroll
+      for (int i = 0; i < kT; ++i) o[t][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      m_ref[t] = kNoKeysYet;
+      l_part[t] = l_exact[t] = 0.0f;
+    }
+
+    auto compute = [&](DecodeRegs<D>& cur, const uint8_t* kbuf, const SharedStep& st) {
+      const int p0 = (int)(st.what0 >> 8) * kPage, p1 = (int)(st.what1 >> 8) * kPage;  // first positions
+      const uint32_t rows = (st.what0 | st.what1) & 0xFF;
+      const bool tail = max(p0, p1) + kPage - 1 > least;  // some key may be past some row's position
+      if (tail) {
+        // V rows past every position must not reach the MFMA (NaN * 0 = NaN)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < DecodeRegs<D>::kLoads; ++i)
+            if ((t ? p1 : p0) + i * kRpl + lane / VL::kNG > last) cur.v[t][i] = zero_u32x4();
+      }
+      f32x4 s[kTiles][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        u32x4 kk[kC];
+#pragma unroll
+        for (int c = 0; c < kC; ++c)
+          kk[c] = *reinterpret_cast<const u32x4*>(kbuf + t * KL::kPageBytes + 1024 * (c >> 1) +
+                                                  ((c & 1) ? k_rd_odd : k_rd_even));
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) {
+          s[u][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int c = 0; c < kC; ++c) s[u][t] = mfma16(as_bf16x8(kk[c]), qf[u][c], s[u][t]);
+        }
+      }
+      uint8_t* vbuf = const_cast<uint8_t*>(kbuf);  // V over the K copy, which is done with
+#pragma unroll
+      for (int hp = 0; hp < 2; ++hp)
+#pragma unroll
+        for (int i = 0; i < DecodeRegs<D>::kLoads; ++i)
+          *reinterpret_cast<u32x4*>(vbuf + hp * KL::kPageBytes + v_wr[i]) = cur.v[hp][i];
+      bf16x8 pb[kTiles];
+#pragma unroll
+      for (int u = 0; u < kTiles; ++u) {
+        if (kTiles > 1 && !(rows & tile_rows[u])) continue;  // no row of this product
+        const bool in0 = (st.what0 & bit[u]) != 0, in1 = st.n1 && (st.what1 & bit[u]) != 0;
+        if (tail) {  // keys past the row's position
+          const int n0 = pos_of[u] - p0 + 1 - 4 * grp, n1 = pos_of[u] - p1 + 1 - 4 * grp;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[u][0][e] = e < n0 ? s[u][0][e] : -INFINITY;
+            s[u][1][e] = e < n1 ? s[u][1][e] : -INFINITY;
+          }
+        }
+        const float top0 = fmaxf(fmaxf(s[u][0][0], s[u][0][1]), fmaxf(s[u][0][2], s[u][0][3]));
+        const float top1 = fmaxf(fmaxf(s[u][1][0], s[u][1][1]), fmaxf(s[u][1][2], s[u][1][3]));
+        float mt = a.scale_log2 * fmaxf(in0 ? top0 : -INFINITY, in1 ? top1 : -INFINITY);
+        if (__any(mt > m_ref[u] + kRescaleSlack)) {  // only then is the column's maximum worked out
+          mt = fmaxf(mt, xor_shfl(mt, 16));
+          mt = fmaxf(mt, xor_shfl(mt, 32));
+          const float m_new = fmaxf(m_ref[u], mt);
+          const float alpha = fast_exp2(m_ref[u] - m_new);
+          l_part[u] *= alpha;
+          l_exact[u] *= alpha;
+#pragma unroll
+          for (int t = 0; t < kT; ++t) o[u][t] *= alpha;
+          m_ref[u] = m_new;
+        }
+        // a row that does not list the block has weights of 2^-inf
+        const float off0 = in0 ? -m_ref[u] : -INFINITY, off1 = in1 ? -m_ref[u] : -INFINITY;
+        u32x4 wp;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float x0 = fast_exp2(fmaf(s[u][t][2 * e], a.scale_log2, t ? off1 : off0));
+            const float x1 = fast_exp2(fmaf(s[u][t][2 * e + 1], a.scale_log2, t ? off1 : off0));
+            // weights go to the P V product in bf16; the sum that divides it is of the rounded ones
+            wp[2 * t + e] = pack_bf16x2(x0, x1);
+            l_part[u] = add_bf16x2(wp[2 * t + e], l_part[u]);
+            l_exact[u] += x0 + x1;
+          }
+        pb[u] = as_bf16x8(wp);
+      }
+#pragma unroll
+      for (int t = 0; t < kT; ++t) {
+        const uint2 v0 = read_tr(vbuf + (v_rd ^ (32 * t))), v1 = read_tr(vbuf + KL::kPageBytes + (v_rd ^ (32 * t)));
+        const bf16x8 vv = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u)
+          if (kTiles == 1 || (rows & tile_rows[u])) o[u][t] = mfma16(vv, pb[u], o[u][t]);
+      }
+    };
+
+    {
+      DecodeRegs<D> ra, rb;
+      SharedStep sa = issue(ra, ka), sb;
+      // no wave reads marks any more, which the loads overwrite
+      while (sa.n0) {
+        sb = issue(rb, kb);
+        __builtin_amdgcn_sched_barrier(0);
+        compute(ra, ka, sa);
+        if (!sb.n0) break;
+        sa = issue(ra, ka);
+        __builtin_amdgcn_sched_barrier(0);
+        compute(rb, kb, sb);
+      }
+    }
+
+    // ---- the waves' parts ----
+    // every load into LDS, the zero-length ones too, is done before LDS takes the parts
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_waitcnt(0);
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    auto sum_cols = [&](float v) {
+      v += xor_shfl(v, 16);
+      return v + xor_shfl(v, 32);
+    };
+    const int l1 = unknown(lane), c1 = l1 & 15, g1 = l1 >> 4;
+#pragma unroll
+    for (int u = 0; u < kTiles; ++u) {
+      const float l = sum_cols(l_part[u]), lx = sum_cols(l_exact[u]);
+      uint8_t* to = u ? kb : ka;
+#pragma unroll
+      for (int t = 0; t < kT; ++t)
+        *reinterpret_cast<f32x4*>(to + 4 * D * c1 + 16 * ((4 * t + g1) ^ c1)) = o[u][t];
+      if (g1 == 0) stats[wave][16 * u + c1] = f32x4{m_ref[u], l, lx, 0.0f};
+    }
+    __syncthreads();
+    const int it = unknown(tid), il = it & 63;
+    // whether a row has a key at all: it lists a block of the pool (every listed block has one)
+    uint32_t listed = 0, with_keys = 0;
+    for (int i = il; i < entries; i += 64) listed |= list_page[i] >= 0 ? list_what[i] & 0xFF : 0u;
+#pragma unroll
+    for (int r = 0; r < kSharedRows; ++r) with_keys |= __any((listed >> r) & 1) ? 1u << r : 0u;
+    constexpr int kPiece = D / 4;  // 16-byte pieces of a head's output
+    uint32_t again = 0;
+    for (int i = it; i < R * G * kPiece; i += kSharedThreads) {
+      const int rh = i / kPiece, p = i % kPiece, r = rh / G, h = rh - r * G;
+      if (!((subset >> r) & 1)) continue;
+      const int c = (r << shift) + h, j = c & 15;
+      const uint8_t* from = (c < 16 ? k_lds0 : k_lds1) + 4 * D * j + 16 * (p ^ j);
+      f32x4 st[kWaves];
+      float m = kNoKeysYet;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        st[w] = stats[w][c];
+        m = fmaxf(m, st[w][0]);
+      }
+      f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      float ls = 0.0f, lxs = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = fast_exp2(st[w][0] - m);
+        acc += f * *reinterpret_cast<const f32x4*>(from + w * 2 * KL::kPageBytes);
+        ls += f * st[w][1];
+        lxs += f * st[w][2];
+      }
+      const bool has = (with_keys >> r) & 1;
+      const float inv = has ? 1.0f / ls : 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (!(fabsf(acc[e] * inv) < INFINITY)) again |= 1u << r;
+      }
+      const int64_t at = (row0 + r) * a.num_q_heads + head * G + h;
+      const uint2 x = {pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+      *reinterpret_cast<uint2*>(a.out + at * D + 4 * p) = has ? x : uint2{0u, 0u};
+      if (a.lse && p == 0) a.lse[at] = has ? (m + __log2f(lxs)) * kLn2 : -INFINITY;
+    }
+    if (again && !alone) atomicOr(&flags, again);
+    __syncthreads();
+    const uint32_t redo = alone ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)flags);
+    left &= ~subset | redo;
+    solo |= redo;
+    __syncthreads();  // flags, marks and parts have been read
+  }
+  if (flag_error) atomicOr(a.error_flags, 1);
+}
+
+template <int D>
+hipError_t launch_shared(const SparseArgs& a, hipStream_t stream) {
+  const uint32_t groups = (uint32_t)((a.rows + a.rows_at_once - 1) / a.rows_at_once);
+  const dim3 grid(groups * (uint32_t)a.num_kv_heads);
+  if ((a.rows_at_once << a.padded_shift) > 16)
+    hipLaunchKernelGGL((sparse_shared_kernel<D, 2>), grid, dim3(kSharedThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((sparse_shared_kernel<D, 1>), grid, dim3(kSharedThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+// Every variant is instantiated explicitly (see attn_decode.hip).
+template __global__ void sparse_shared_kernel<128, 1>(SparseArgs);
+template __global__ void sparse_shared_kernel<128, 2>(SparseArgs);
+template __global__ void sparse_shared_kernel<64, 1>(SparseArgs);
+template __global__ void sparse_shared_kernel<64, 2>(SparseArgs);
+
+}  // namespace kern
+
+hipError_t launch_sparse_shared(const SparseArgs& a, int head_dim, hipStream_t stream) {
+  return head_dim == 128 ? kern::launch_shared<128>(a, stream) : kern::launch_shared<64>(a, stream);
+}
+
+}  // namespace tide

@@ -591,6 +591,11 @@ struct BlockSelectArgs {
   int32_t* error_flags;
 };
 
+// Rows taken together by the shared kernel: entries of its packed list, and blocks of a context that it can mark.
+constexpr int kSharedEntries = 1536, kSharedRows = 8;
+template <int D>
+constexpr int kSharedBlocks = 8 * kPage * D * 2;
+
 struct SparseArgs {
   const uint16_t* q;
   const uint16_t* k_pool;
@@ -609,6 +614,7 @@ struct SparseArgs {
   const int32_t* sel;
   int32_t budget;
   int32_t splits;       // workgroups that share a (row, kv head)
+  int32_t rows_at_once, padded_shift;  // shared kernel: rows of a workgroup, log2 of the columns of each
   float* part_o;        // [rows of a launch][Hkv][splits][group][d]
   float* part_ml;       // [..][splits][group][4]: max (base-2 units), sum of the bf16-rounded weights,
                         // exact sum, 1 if the part has a key
