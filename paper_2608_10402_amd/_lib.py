@@ -720,11 +720,25 @@ def tide_rows_workspace_size(op: int, num_rows: int, dims: tide_dims, budget: in
     return int(out.value)
 
 
+# A step of these calls is a few microseconds of GPU time, so what passes is checked in one look at each tensor.
+_BF16, _I8, _I32T, _I64T, _F32 = torch.bfloat16, torch.int8, torch.int32, torch.int64, torch.float32
+
+
+def _ptr(t, dtype, dev, name):
+    """The address of a contiguous tensor of this type on device `dev`; else the error that says why not."""
+    if isinstance(t, torch.Tensor):
+        if t.dtype is dtype and t.get_device() == dev and dev >= 0 and t.is_contiguous():
+            return t.data_ptr()
+        if dev >= 0 and t.get_device() >= 0 and t.get_device() != dev:
+            raise ValueError("all tensors of a call must be on one device, got %s for %s" % (t.device, name))
+    return _dev(t, dtype, name)
+
+
 def _vector(t, name, n):
     """t must be a 1-D tensor of n entries."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
-    if t.dim() != 1 or t.shape[0] != n:
+    if t.shape != (n,):
         raise ValueError("%s must have shape (%d,), got %s" % (name, n, tuple(t.shape)))
 
 
@@ -735,32 +749,34 @@ def _count_of(t, name):
 
 
 def _bounds_pools(bounds, units, num_pages, dims):
-    shape = (num_pages, dims.num_kv_heads, 2, dims.head_dim)
-    if tuple(bounds.shape) != shape:
-        raise ValueError("bounds must have shape %s, got %s" % (shape, tuple(bounds.shape)))
-    if tuple(units.shape) != shape[:2]:
-        raise ValueError("units must have shape %s, got %s" % (shape[:2], tuple(units.shape)))
+    heads, d = dims.num_kv_heads, dims.head_dim
+    if bounds.shape != (num_pages, heads, 2, d):
+        raise ValueError("bounds must have shape %s, got %s" % ((num_pages, heads, 2, d), tuple(bounds.shape)))
+    if units.shape != (num_pages, heads):
+        raise ValueError("units must have shape %s, got %s" % ((num_pages, heads), tuple(units.shape)))
 
 
 def tide_page_map(lens, want_lens, block_table, free_pages, free_count, lens_out, free_count_out, row_start,
                   row_task, row_pos, row_slot, dims: tide_dims, stream=None) -> None:
     """All of them device tensors: int32, row_slot int64."""
     n, rows = _count_of(lens, "lens"), _count_of(row_task, "row_task")
-    for t, name, m in ((want_lens, "want_lens", n), (lens_out, "lens_out", n), (free_count, "free_count", 1),
-                       (free_count_out, "free_count_out", 1), (row_start, "row_start", n + 1),
-                       (row_pos, "row_pos", rows), (row_slot, "row_slot", rows)):
-        _vector(t, name, m)
+    _vector(want_lens, "want_lens", n)
+    _vector(lens_out, "lens_out", n)
+    _vector(free_count, "free_count", 1)
+    _vector(free_count_out, "free_count_out", 1)
+    _vector(row_start, "row_start", n + 1)
+    _vector(row_pos, "row_pos", rows)
+    _vector(row_slot, "row_slot", rows)
     stride = _block_table(block_table, n)
     capacity = _count_of(free_pages, "free_pages")
-    _same_device(lens, want_lens, block_table, free_pages, free_count, lens_out, free_count_out, row_start,
-                 row_task, row_pos, row_slot)
-    i32 = torch.int32
+    dev = lens.get_device()
     _invoke("tide_page_map", lens, stream,
-            _dev(lens, i32, "lens"), _dev(want_lens, i32, "want_lens"), n, _dev(block_table, i32, "block_table"),
-            int(stride), _dev(free_pages, i32, "free_pages"), capacity, _dev(free_count, i32, "free_count"), rows,
-            _dev(lens_out, i32, "lens_out"), _dev(free_count_out, i32, "free_count_out"),
-            _dev(row_start, i32, "row_start"), _dev(row_task, i32, "row_task"), _dev(row_pos, i32, "row_pos"),
-            _dev(row_slot, torch.int64, "row_slot"), ctypes.byref(dims))
+            _ptr(lens, _I32T, dev, "lens"), _ptr(want_lens, _I32T, dev, "want_lens"), n,
+            _ptr(block_table, _I32T, dev, "block_table"), stride, _ptr(free_pages, _I32T, dev, "free_pages"), capacity,
+            _ptr(free_count, _I32T, dev, "free_count"), rows, _ptr(lens_out, _I32T, dev, "lens_out"),
+            _ptr(free_count_out, _I32T, dev, "free_count_out"), _ptr(row_start, _I32T, dev, "row_start"),
+            _ptr(row_task, _I32T, dev, "row_task"), _ptr(row_pos, _I32T, dev, "row_pos"),
+            _ptr(row_slot, _I64T, dev, "row_slot"), ctypes.byref(dims))
 
 
 def tide_slot_append(k_new, v_new, row_slot, k_pool, v_pool, dims: tide_dims, bounds=None, units=None,
@@ -771,32 +787,34 @@ def tide_slot_append(k_new, v_new, row_slot, k_pool, v_pool, dims: tide_dims, bo
     _rows(v_new, "v_new", rows, dims.num_kv_heads, dims.head_dim)
     if (bounds is None) != (units is None):
         raise ValueError("bounds and units go together")
+    dev, b, u = k_pool.get_device(), None, None
     if bounds is not None:
         _bounds_pools(bounds, units, num_pages, dims)
-    _same_device(k_new, v_new, row_slot, k_pool, v_pool, bounds, units, workspace)
+        b, u = _ptr(bounds, _I8, dev, "bounds"), _ptr(units, _I8, dev, "units")
     ws, ws_n = _ws(workspace)
+    _same_device(k_pool, workspace)
     _invoke("tide_slot_append", k_pool, stream,
-            _dev(k_new, torch.bfloat16, "k_new"), _dev(v_new, torch.bfloat16, "v_new"),
-            _dev(row_slot, torch.int64, "row_slot"), rows, _dev(k_pool, torch.bfloat16, "k_pool"),
-            _dev(v_pool, torch.bfloat16, "v_pool"), num_pages, _dev(bounds, torch.int8, "bounds", nullable=True),
-            _dev(units, torch.int8, "units", nullable=True), ctypes.byref(dims), ws, ws_n)
+            _ptr(k_new, _BF16, dev, "k_new"), _ptr(v_new, _BF16, dev, "v_new"), _ptr(row_slot, _I64T, dev, "row_slot"),
+            rows, _ptr(k_pool, _BF16, dev, "k_pool"), _ptr(v_pool, _BF16, dev, "v_pool"), num_pages, b, u,
+            ctypes.byref(dims), ws, ws_n)
 
 
 def tide_key_bounds(k_pool, block_table, lens, bounds, units, dims: tide_dims, from_lens=None, max_len: int = 0,
                     workspace=None, stream=None) -> None:
     num_pages = _pool_shape(k_pool, k_pool, dims)
     n = _count_of(lens, "lens")
+    dev, start = k_pool.get_device(), None
     if from_lens is not None:
         _vector(from_lens, "from_lens", n)
+        start = _ptr(from_lens, _I32T, dev, "from_lens")
     _bounds_pools(bounds, units, num_pages, dims)
     stride = _block_table(block_table, n)
-    _same_device(k_pool, block_table, lens, from_lens, bounds, units, workspace)
     ws, ws_n = _ws(workspace)
+    _same_device(k_pool, workspace)
     _invoke("tide_key_bounds", k_pool, stream,
-            _dev(k_pool, torch.bfloat16, "k_pool"), num_pages, _dev(block_table, torch.int32, "block_table"),
-            int(stride), n, _dev(lens, torch.int32, "lens"), _dev(from_lens, torch.int32, "from_lens", nullable=True),
-            int(max_len), _dev(bounds, torch.int8, "bounds"), _dev(units, torch.int8, "units"), ctypes.byref(dims),
-            ws, ws_n)
+            _ptr(k_pool, _BF16, dev, "k_pool"), num_pages, _ptr(block_table, _I32T, dev, "block_table"), stride, n,
+            _ptr(lens, _I32T, dev, "lens"), start, max_len, _ptr(bounds, _I8, dev, "bounds"),
+            _ptr(units, _I8, dev, "units"), ctypes.byref(dims), ws, ws_n)
 
 
 def tide_block_select(q, row_task, row_pos, bounds, units, block_table, budget: int, dims: tide_dims, sel,
@@ -806,18 +824,18 @@ def tide_block_select(q, row_task, row_pos, bounds, units, block_table, budget: 
     _rows(q, "q", rows, dims.num_q_heads, dims.head_dim)
     num_pages = bounds.shape[0]
     _bounds_pools(bounds, units, num_pages, dims)
-    if tuple(sel.shape) != (rows, dims.num_kv_heads, budget):
+    if sel.shape != (rows, dims.num_kv_heads, budget):
         raise ValueError("sel must have shape (%d, %d, %d), got %s"
                          % (rows, dims.num_kv_heads, budget, tuple(sel.shape)))
     stride = _block_table(block_table, 0)
-    _same_device(q, row_task, row_pos, bounds, units, block_table, sel, workspace)
+    dev = q.get_device()
     ws, ws_n = _ws(workspace)
+    _same_device(q, workspace)
     _invoke("tide_block_select", q, stream,
-            _dev(q, torch.bfloat16, "q"), _dev(row_task, torch.int32, "row_task"),
-            _dev(row_pos, torch.int32, "row_pos"), rows, _dev(bounds, torch.int8, "bounds"),
-            _dev(units, torch.int8, "units"), num_pages, _dev(block_table, torch.int32, "block_table"),
-            int(stride), int(block_table.shape[0]), int(budget), int(sink), int(recent), int(max_len),
-            ctypes.byref(dims), _dev(sel, torch.int32, "sel"), ws, ws_n)
+            _ptr(q, _BF16, dev, "q"), _ptr(row_task, _I32T, dev, "row_task"), _ptr(row_pos, _I32T, dev, "row_pos"),
+            rows, _ptr(bounds, _I8, dev, "bounds"), _ptr(units, _I8, dev, "units"), num_pages,
+            _ptr(block_table, _I32T, dev, "block_table"), stride, block_table.shape[0], budget, sink, recent, max_len,
+            ctypes.byref(dims), _ptr(sel, _I32T, dev, "sel"), ws, ws_n)
 
 
 def tide_sparse_attn(q, k_pool, v_pool, block_table, row_task, row_pos, sel, dims: tide_dims, out, lse=None,
@@ -828,18 +846,18 @@ def tide_sparse_attn(q, k_pool, v_pool, block_table, row_task, row_pos, sel, dim
     _rows(q, "q", rows, dims.num_q_heads, dims.head_dim)
     _rows(out, "out", rows, dims.num_q_heads, dims.head_dim)
     _lse(lse, rows, dims.num_q_heads)
-    if sel.dim() != 3 or tuple(sel.shape[:2]) != (rows, dims.num_kv_heads):
+    if sel.dim() != 3 or sel.shape[0] != rows or sel.shape[1] != dims.num_kv_heads:
         raise ValueError("sel must be [%d][%d][budget], got %s" % (rows, dims.num_kv_heads, tuple(sel.shape)))
     stride = _block_table(block_table, 0)
-    _same_device(q, k_pool, v_pool, block_table, row_task, row_pos, sel, out, lse, workspace)
+    dev = k_pool.get_device()
     ws, ws_n = _ws(workspace)
+    _same_device(k_pool, workspace)
     _invoke("tide_sparse_attn", k_pool, stream,
-            _dev(q, torch.bfloat16, "q"), _dev(k_pool, torch.bfloat16, "k_pool"),
-            _dev(v_pool, torch.bfloat16, "v_pool"), num_pages, _dev(block_table, torch.int32, "block_table"),
-            int(stride), int(block_table.shape[0]), _dev(row_task, torch.int32, "row_task"),
-            _dev(row_pos, torch.int32, "row_pos"), rows, _dev(sel, torch.int32, "sel"), int(sel.shape[2]),
-            ctypes.byref(dims), _dev(out, torch.bfloat16, "out"), _dev(lse, torch.float32, "lse", nullable=True),
-            ws, ws_n)
+            _ptr(q, _BF16, dev, "q"), _ptr(k_pool, _BF16, dev, "k_pool"), _ptr(v_pool, _BF16, dev, "v_pool"), num_pages,
+            _ptr(block_table, _I32T, dev, "block_table"), stride, block_table.shape[0],
+            _ptr(row_task, _I32T, dev, "row_task"), _ptr(row_pos, _I32T, dev, "row_pos"), rows,
+            _ptr(sel, _I32T, dev, "sel"), sel.shape[2], ctypes.byref(dims), _ptr(out, _BF16, dev, "out"),
+            None if lse is None else _ptr(lse, _F32, dev, "lse"), ws, ws_n)
 
 
 def tide_shutdown() -> None:

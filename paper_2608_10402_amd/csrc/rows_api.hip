@@ -60,15 +60,16 @@ SelectRounds select_rounds(int32_t num_rows, int32_t max_len, const tide_dims& d
   return r;
 }
 
-// ---- sparse attention: workgroups that share a (row, kv head) where there are few of them
-constexpr int32_t kSparseGroups = 512;     // that the device holds at once
-constexpr int32_t kLeastPairs = 8;         // pairs of blocks of a workgroup: two a wave
+// ---- sparse attention: workgroups that share a (row, kv head) where there are few of them.  A part keeps 8 steps for
+// each of its 8 waves: less does not pay for the second kernel, which joins the parts (4 rows of 64 blocks and 4 kv
+// heads: 6.4 + 4 us in four parts, 10.6 in one, and a launch less).
+constexpr int32_t kLeastPairs = 64;
 constexpr int32_t kSparseLaunch = 1 << 23; // workgroups of a launch (fewer than 2^32 threads)
 
 int32_t sparse_splits(int64_t num_rows, int32_t budget, const tide_dims& dims) {
   const int64_t units = num_rows * dims.num_kv_heads;
   const int64_t pairs = ((int64_t)budget + 1) / 2;
-  return (int32_t)std::max<int64_t>(1, std::min(kSparseGroups / units, pairs / kLeastPairs));
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSparseAlone / units, pairs / kLeastPairs));
 }
 
 size_t sparse_bytes(int32_t num_rows, int32_t budget, const tide_dims& dims, size_t* ml_off) {

@@ -23,14 +23,15 @@ namespace kern {
 // score but -inf.
 constexpr float kNoKeys = -3.0e38f;
 
-constexpr int kSparseWaves = 4;
+// Waves of a workgroup: 8 where its workgroups leave CUs idle (kWide), 4 else.
+constexpr int kSparseWide = 8, kSparseWaves = 4;
 
-template <int D, int kPolicy>
-__global__ __launch_bounds__(kSparseWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+template <int D, int kPolicy, int kWaves>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void sparse_attn_kernel(SparseArgs a) {
   using KL = KLds<D>;
   using VL = VLds<D>;
-  constexpr int kC = D / 32, kT = D / 16, kWaves = kSparseWaves;
+  constexpr int kC = D / 32, kT = D / 16;
   const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hkv = a.num_kv_heads, G = a.group;
@@ -302,19 +303,35 @@ __global__ __launch_bounds__(256) void sparse_merge_kernel(SparseArgs a) {
   if (a.lse && p == 0) a.lse[at] = has > 0.0f ? (m + __log2f(lx)) * kLn2 : -INFINITY;
 }
 
+template <int D, int kPolicy>
+void launch_lists(const SparseArgs& a, hipStream_t stream) {
+  const uint32_t groups = (uint32_t)a.rows * (uint32_t)a.num_kv_heads * (uint32_t)a.splits;
+  if (groups <= kSparseAlone)
+    hipLaunchKernelGGL((sparse_attn_kernel<D, kPolicy, kSparseWide>), dim3(groups), dim3(kSparseWide * 64), 0, stream, a);
+  else
+    hipLaunchKernelGGL((sparse_attn_kernel<D, kPolicy, kSparseWaves>), dim3(groups), dim3(kSparseWaves * 64), 0, stream, a);
+}
+
 template <int D>
 hipError_t launch_sparse_d(const SparseArgs& a, bool shared, hipStream_t stream) {
-  const dim3 grid((uint32_t)a.rows * (uint32_t)a.num_kv_heads * (uint32_t)a.splits);
-  if (shared)
-    hipLaunchKernelGGL((sparse_attn_kernel<D, kSharedPolicy>), grid, dim3(kSparseWaves * 64), 0, stream, a);
-  else
-    hipLaunchKernelGGL((sparse_attn_kernel<D, kStreamPolicy>), grid, dim3(kSparseWaves * 64), 0, stream, a);
+  if (shared) launch_lists<D, kSharedPolicy>(a, stream);
+  else launch_lists<D, kStreamPolicy>(a, stream);
   const hipError_t rc = hipGetLastError();
   if (rc != hipSuccess || a.splits == 1) return rc;
   const int64_t threads = (int64_t)a.rows * a.num_q_heads * (D / 4);
   hipLaunchKernelGGL((sparse_merge_kernel<D>), dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
+
+// Every variant is instantiated explicitly (see attn_decode.hip).
+template __global__ void sparse_attn_kernel<128, kSharedPolicy, kSparseWide>(SparseArgs);
+template __global__ void sparse_attn_kernel<128, kSharedPolicy, kSparseWaves>(SparseArgs);
+template __global__ void sparse_attn_kernel<128, kStreamPolicy, kSparseWide>(SparseArgs);
+template __global__ void sparse_attn_kernel<128, kStreamPolicy, kSparseWaves>(SparseArgs);
+template __global__ void sparse_attn_kernel<64, kSharedPolicy, kSparseWide>(SparseArgs);
+template __global__ void sparse_attn_kernel<64, kSharedPolicy, kSparseWaves>(SparseArgs);
+template __global__ void sparse_attn_kernel<64, kStreamPolicy, kSparseWide>(SparseArgs);
+template __global__ void sparse_attn_kernel<64, kStreamPolicy, kSparseWaves>(SparseArgs);
 
 }  // namespace kern
 

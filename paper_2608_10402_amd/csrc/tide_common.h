@@ -596,6 +596,9 @@ constexpr int kSharedEntries = 1536, kSharedRows = 8;
 template <int D>
 constexpr int kSharedBlocks = 8 * kPage * D * 2;
 
+// Workgroups of a call up to which each has a CU of its own, and takes 8 waves.
+constexpr uint32_t kSparseAlone = 256;
+
 struct SparseArgs {
   const uint16_t* q;
   const uint16_t* k_pool;

@@ -204,16 +204,15 @@ class PagedKV(_Paged):
         """Store the rows' K/V in their slots (tide_slot_append); with bounds, bring those of the
         pages that change up to date."""
         b, u = bounds if bounds is not None else (None, None)
-        self._call(lambda: _lib.tide_rows_workspace_size(_lib.TIDE_OP_SLOT_APPEND, row_slot.numel(), self.dims),
-                   lambda ws: _lib.tide_slot_append(k_new, v_new, row_slot, self.k_pool, self.v_pool, self.dims, b, u,
-                                                    ws, stream))
+        # (the smallest workspace there is holds the error flags, which is all these two calls need)
+        _lib.tide_slot_append(k_new, v_new, row_slot, self.k_pool, self.v_pool, self.dims, b, u,
+                              self._ws if self._ws is not None else self.workspace(0), stream)
 
     def key_bounds(self, lens, bounds, from_lens=None, max_len: int = 0, stream=None):
         """Key bounds of the pages that hold positions from_lens (None: 0) .. lens - 1 of each task, both on
         the device (tide_key_bounds): after append, extend_append, evict and what else writes keys."""
-        self._call(lambda: _lib.tide_rows_workspace_size(_lib.TIDE_OP_KEY_BOUNDS, lens.numel(), self.dims),
-                   lambda ws: _lib.tide_key_bounds(self.k_pool, self.block_table, lens, bounds[0], bounds[1],
-                                                   self.dims, from_lens, max_len, ws, stream))
+        _lib.tide_key_bounds(self.k_pool, self.block_table, lens, bounds[0], bounds[1], self.dims, from_lens, max_len,
+                             self._ws if self._ws is not None else self.workspace(0), stream)
         return bounds
 
     def select_blocks(self, q, row_task, row_pos, bounds, budget: int, sink: int = 0, recent: int = 0,
