@@ -813,7 +813,7 @@ def tide_key_bounds(k_pool, block_table, lens, bounds, units, dims: tide_dims, f
     _same_device(k_pool, workspace)
     _invoke("tide_key_bounds", k_pool, stream,
             _ptr(k_pool, _BF16, dev, "k_pool"), num_pages, _ptr(block_table, _I32T, dev, "block_table"), stride, n,
-            _ptr(lens, _I32T, dev, "lens"), start, max_len, _ptr(bounds, _I8, dev, "bounds"),
+            _ptr(lens, _I32T, dev, "lens"), start, int(max_len), _ptr(bounds, _I8, dev, "bounds"),
             _ptr(units, _I8, dev, "units"), ctypes.byref(dims), ws, ws_n)
 
 
@@ -834,7 +834,8 @@ def tide_block_select(q, row_task, row_pos, bounds, units, block_table, budget: 
     _invoke("tide_block_select", q, stream,
             _ptr(q, _BF16, dev, "q"), _ptr(row_task, _I32T, dev, "row_task"), _ptr(row_pos, _I32T, dev, "row_pos"),
             rows, _ptr(bounds, _I8, dev, "bounds"), _ptr(units, _I8, dev, "units"), num_pages,
-            _ptr(block_table, _I32T, dev, "block_table"), stride, block_table.shape[0], budget, sink, recent, max_len,
+            _ptr(block_table, _I32T, dev, "block_table"), stride, block_table.shape[0], int(budget), int(sink),
+            int(recent), int(max_len),
             ctypes.byref(dims), _ptr(sel, _I32T, dev, "sel"), ws, ws_n)
 
 

@@ -148,7 +148,9 @@ def rows_of(prefix, extend):
 
 APPEND = [  # prefix, extend, kv heads, d
     ([0], [1], 1, 64), ([15], [1], 2, 128), ([3, 0, 40], [5, 33, 0], 4, 128), ([7, 16, 31], [60, 16, 2], 5, 64),
-    ([1000], [129], 3, 128), ([0] * 40, [17] * 40, 1, 128), (list(range(33)), [1] * 33, 8, 128), ([14], [4], 64, 64)]
+    ([1000], [129], 3, 128), ([0] * 40, [17] * 40, 1, 128), (list(range(33)), [1] * 33, 8, 128), ([14], [4], 64, 64),
+    # more rows x kv heads than are taken one by one: windows of 16 rows, few and many first rows of pages in each
+    ([5, 100], [210, 61], 64, 64), (list(range(70, 370)), [1] * 300, 64, 64), ([3] * 37, [7] * 37, 65, 128)]
 
 
 @pytest.mark.parametrize("prefix,extend,hkv,d", APPEND)
@@ -415,13 +417,13 @@ class Sparse:
                 sel[r, h, self.rng.permutation(budget)[: pick.size]] = pick
         return sel
 
-    def check(self, q, task, pos, sel, want_lse=True, live=None):
+    def check(self, q, task, pos, sel, want_lse=True, live=None, only=None):
         n, g = len(task), self.hq // self.hkv
         out = torch.full((n, self.hq, self.d), 7.0, dtype=torch.bfloat16, device="cuda")
         lse = torch.full((n, self.hq), 7.0, device="cuda") if want_lse else None
         self.p.kv.sparse(rows_to_dev(q), dev(task), dev(pos), dev(sel), out=out, lse=lse)
         got, got_lse = host(out), None if lse is None else host(lse)
-        for r in range(n):
+        for r in range(n) if only is None else only:
             if live is not None and not live[r]:
                 assert (got[r] == 7.0).all() and (lse is None or (got_lse[r] == 7.0).all())
                 continue
@@ -460,6 +462,77 @@ def test_attention_over_long_lists(rows, budget):
     sel = s.lists(task, pos, budget)
     sel[0, :, :] = s.rng.permutation(1200)[:budget]
     s.check(q, task, pos, sel)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 8, 128), (14, 2, 64)])
+def test_attention_of_a_row_a_task(hq, hkv, d):
+    """A decode batch: as many tasks as rows, too many to split."""
+    n = 300 if hkv < 8 else 70
+    s = Sparse(21, list(np.random.default_rng(21).integers(1, 700, n)), hq, hkv, d)
+    q, _, _ = s.rows(n)
+    task, pos = np.arange(n), np.array(s.lens) - 1
+    s.check(q, task, pos, s.lists(task, pos, 11))
+
+
+@pytest.mark.parametrize("hq,hkv", [(32, 4), (1, 1), (4, 2), (16, 1)])
+@pytest.mark.parametrize("budget", [1, 2, 40, 192])
+def test_rows_taken_together(hq, hkv, budget):
+    """Runs of rows of one task whose lists overlap much, little and not at all, with rows of other tasks and
+    padding between; enough of them that none is split."""
+    s = Sparse(hq + budget, [4000, 700, 3300], hq, hkv, 128)
+    n = 600 // hkv
+    q, task, pos = s.rows(n)
+    task[: n // 2], pos[: n // 2] = 0, 3400 + np.arange(n // 2)
+    sel = s.lists(task, pos, budget)
+    for r in range(n // 2):  # neighbours differ in a few blocks; each has its own last one
+        common = np.random.default_rng(r // 16).permutation(200)[:budget]
+        sel[r] = common
+        own = s.rng.permutation(np.setdiff1d(np.arange(212), common))[: budget // 8]
+        sel[r, :, : own.size] = own
+        sel[r, :, budget - 1] = pos[r] // PAGE
+    live = np.ones(n, bool)
+    for i, (t, p) in ((3, (-1, 9)), (17, (0, -4)), (n // 2 + 1, (3, 0))):
+        task[i], pos[i], live[i] = t, p, False
+    some = sorted(set(s.rng.permutation(n)[:60]) | set(range(20)) | {n // 2 + 1, n - 1})  # all are computed
+    s.check(q, task, pos, sel, live=live, only=some)
+
+
+def test_rows_taken_together_that_list_a_block_twice():
+    s = Sparse(31, [3000], 8, 1, 64)
+    q, task, pos = s.rows(600)
+    pos[:] = 2000 + np.arange(600)
+    sel = np.tile(np.arange(20), (600, 1, 1))
+    sel[5, 0, 7] = 3           # block 3 twice in row 5 alone
+    sel[64:72, 0, 1] = 0       # and in all rows of a group
+    s.check(q, task, pos, sel, only=range(90))
+
+
+def test_rows_taken_together_do_not_share_what_is_not_a_number():
+    """V and K that are not finite in blocks that some rows of a group list, and past the position of some."""
+    s = Sparse(32, [3000], 8, 1, 128)
+    q, task, pos = s.rows(600)
+    pos[:] = 2000 + np.arange(600)
+    sel = np.tile(np.arange(20), (600, 1, 1))
+    sel[:, 0, 19] = pos // PAGE
+    sel[2, 0, 4], sel[3, 0, 5], sel[9, 0, 6] = 40, 41, 42
+    for b, x in ((40, np.nan), (41, np.inf), (42, -np.inf)):
+        s.p.v[s.table[0, b], 0, 3, 5] = x
+        s.p.k[s.table[0, b], 0, 9, 7] = x
+    at = 2013  # position of row 13: rows 8 .. 12 of its group of 8 or 4 list the block and do not see it
+    s.p.v[s.table[0, at // PAGE], 0, at % PAGE, 1] = np.inf
+    s.upload()
+    out = host(s.p.kv.sparse(rows_to_dev(q), dev(task), dev(pos), dev(sel)))
+    bad = {r for r in range(600) if not np.isfinite(out[r]).all()}
+    assert bad == {2, 3, 9} | {r for r in range(13, 600) if pos[r] // PAGE == at // PAGE}
+    s.check(q, task, pos, sel, want_lse=False, only=[0, 1, 4, 8, 10, 12, 40, 599])
+
+
+@pytest.mark.parametrize("budget", [300, 900])
+def test_lists_too_long_to_take_rows_together(budget):
+    s = Sparse(33, [16 * 1000], 8, 1, 128)
+    q, task, pos = s.rows(600)
+    sel = s.lists(task, pos, budget)
+    s.check(q, task, pos, sel, only=range(0, 600, 29))
 
 
 def test_rows_that_see_nothing_and_padding():
