@@ -22,7 +22,9 @@
  *   and decode for GRPO groups whose trajectories share a prompt prefix:
  *     tide_decode_attn_shared tide_decode_attn, reading each shared prefix once per group
  *   The same steps over a cache held in 4 bits (tide_kv4_*), and the eviction of the positions that a
- *   task's queries attended to least (tide_attn_mass, tide_kv_evict).
+ *   task's queries attended to least (tide_attn_mass, tide_kv_evict).  Steps whose lengths live on the device
+ *   (tide_page_map, tide_slot_append), and attention over the blocks of a context that a row's query scores
+ *   highest (tide_key_bounds, tide_block_select, tide_sparse_attn).
  *
  *   The attention itself is standard scaled dot-product attention (Vaswani et al.,
  *   2017), which the paper uses but does not restate: for a query row at absolute
@@ -49,7 +51,8 @@
  *                    k_new/v_new: bf16 [rows][num_kv_heads][head_dim];
  *                    lse: fp32 [rows][num_q_heads] (may be NULL).
  *   lengths          HOST arrays of int32, read synchronously during the call (the
- *                    scheduler that owns task footprints lives on the host, Section 4.1).
+ *                    scheduler that owns task footprints lives on the host, Section 4.1);
+ *                    device arrays in the calls of the last section, which say so.
  *   workspace        device scratch owned by the caller, at least tide_workspace_size()
  *                    bytes; it must not be shared by two calls in flight at once.
  *   stream           a hipStream_t passed as void*; NULL means the default stream.
@@ -522,7 +525,7 @@ TIDE_API int tide_page_map(const int32_t* lens, const int32_t* want_lens, int32_
  * range.  With bounds and units (both or neither NULL) the key bounds of the pages that changed are
  * brought up to date; that takes the page's slots before the new ones to hold keys of the same
  * task, and a page's new rows to follow each other in slot order (the rows of tide_page_map do;
- * otherwise the page's bounds are unspecified).  Two rows of one slot: either's.
+ * otherwise the page's bounds are unspecified).  Two rows of one slot are not ordered: it holds parts of either.
  */
 TIDE_API int tide_slot_append(const void* k_new, const void* v_new, const int64_t* row_slot, int32_t num_rows,
                      void* k_pool, void* v_pool, int64_t num_pages, int8_t* bounds, int8_t* units,
@@ -563,7 +566,8 @@ TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int
 /*
  * Attention of each row over the positions at or before its own in the blocks that sel[row][KV head] lists,
  * in any order; an entry that is negative, past the row's position or whose page id is out of range
- * adds nothing, and a block listed twice counts twice.  q/out: bf16 [num_rows][Hq][d]; lse: fp32
+ * adds nothing, and a block listed twice counts twice.  budget <= 2^30 (TIDE_ERR_UNSUPPORTED; so for
+ * tide_block_select).  q/out: bf16 [num_rows][Hq][d]; lse: fp32
  * [num_rows][Hq] or NULL.  A row of which no entry adds anything gets zeros, and an lse of -inf.
  */
 TIDE_API int tide_sparse_attn(const void* q, const void* k_pool, const void* v_pool, int64_t num_pages,

@@ -295,7 +295,8 @@ void score_rows_kernel(BlockSelectArgs a) {
   const int task = ((const const_i32*)a.row_task)[a.first_row + row], pos = ((const const_i32*)a.row_pos)[a.first_row + row];
   const int blocks = pos / kPage + 1, jump = a.splits * kScoreChunk;
   int b0 = split * kScoreChunk;
-  if (!live_row(task, pos, a.num_tasks, a.max_len) || b0 >= blocks) return;
+  // (a context within the budget is taken whole)
+  if (!live_row(task, pos, a.num_tasks, a.max_len) || b0 >= blocks || blocks <= a.budget) return;
   const int32_t* table = a.block_table + (int64_t)task * a.bt_stride;
   const uint32_t pages = (uint32_t)min(a.num_pages, (int64_t)1 << 31);
   const uint32_t block_bytes = (uint32_t)Hkv * (2 * D);
@@ -540,9 +541,9 @@ int padded_shift(int32_t group) {
 // at most the want-th largest score, so the quads that reach it hold all that is taken, and are few more than
 // `want`: the others are looked at once.  Bins of equal width find it, and then the want-th largest score of the
 // listed quads, with equal scores ranked by position; what is taken becomes bits, which are packed in order.
-// Scores that this does not fit (infinite ones, hundreds of equal ones at the border, budgets above 180 blocks or
-// a quarter of the context, contexts above 262,144) take a way that any can go: bins of keys that narrow to the
-// last key taken, and prefix sums over all.
+// Where the budget is above a quarter of the context all quads are listed.  What this does not fit (more than 256
+// quads to list, infinite scores, more than 64 scores in the border's bin, contexts above 262,144) takes a way that
+// any can go: bins of keys that narrow to the last key taken, and prefix sums over all.
 constexpr int kChooseBins = 512;
 constexpr int kChooseQuads = 256;  // of the list
 constexpr int kChooseWords = 512;  // of bits

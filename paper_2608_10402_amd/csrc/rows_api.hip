@@ -37,6 +37,9 @@ int longest(int32_t max_len, int32_t bt_stride, int32_t* out) {
   return TIDE_OK;
 }
 
+// Entries of a row's list: two rounds of them more still fit in 32 bits.
+constexpr int32_t kMostBudget = 1 << 30;
+
 // ---- selection: rows go in rounds of at most kScoreBytes of scores, which stay in the last-level cache
 constexpr int64_t kScoreBytes = 256 << 20;
 constexpr int32_t kRoundPairs = 1 << 20;  // (row, kv head) pairs of a round
@@ -118,6 +121,7 @@ TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, 
         return TIDE_OK;
       case TIDE_OP_SPARSE_ATTN:
         if (budget <= 0) return TIDE_ERR_INVALID_ARG;
+        if (budget > kMostBudget) return TIDE_ERR_UNSUPPORTED;
         *bytes_out = num_rows ? sparse_bytes(num_rows, budget, *dims, &ml_off) : kHeader;
         return TIDE_OK;
       default:
@@ -246,6 +250,7 @@ TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int
     if (rc != TIDE_OK) return rc;
     if (budget <= 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > budget || num_tasks < 0)
       return TIDE_ERR_INVALID_ARG;
+    if (budget > kMostBudget) return TIDE_ERR_UNSUPPORTED;
     if (!go || num_tasks == 0) return TIDE_OK;
     if (bt_stride <= 0) return TIDE_ERR_INVALID_ARG;
     int32_t most;
@@ -308,6 +313,7 @@ TIDE_API int tide_sparse_attn(const void* q, const void* k_pool, const void* v_p
     int rc = begin(dims, num_rows, num_pages, &go);
     if (rc != TIDE_OK) return rc;
     if (budget <= 0 || num_tasks < 0) return TIDE_ERR_INVALID_ARG;
+    if (budget > kMostBudget) return TIDE_ERR_UNSUPPORTED;
     if (!go || num_tasks == 0) return TIDE_OK;
     if (bt_stride <= 0) return TIDE_ERR_INVALID_ARG;
     if (!q || !k_pool || !v_pool || !block_table || !row_task || !row_pos || !sel || !out || !workspace)

@@ -369,6 +369,17 @@ def test_choice_up_to_max_len():
         c.check(c.queries(3), np.arange(3), pos, 4, 1, 1, max_len, live=pos < (max_len or 10**9))
 
 
+@pytest.mark.parametrize("many", [False, True])
+def test_choice_of_contexts_within_the_budget_and_beyond(many):
+    """Rows whose blocks are all taken beside rows that choose; one row a task, and many."""
+    lens = [16, 150, 176, 177, 160, 1700, 161, 700]
+    c = Choice(10, lens, 8, 2, 128)
+    task = np.arange(8) if not many else c.rng.integers(0, 8, 70)
+    pos = np.array(lens)[task] - 1
+    c.check(c.queries(task.size), task, pos, 10, 1, 2)
+    c.check(c.queries(task.size), task, pos, 11, 0, 0)
+
+
 def test_choice_in_rounds():
     """A table so wide that the rows' scores go through the workspace in rounds."""
     c = Choice(9, [1000, 700], 8, 8, 64)
@@ -724,6 +735,70 @@ def test_another_stream():
         torch.cuda.synchronize()
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+def test_pools_past_32_bits():
+    """Pages, slots and bounds whose offsets do not fit in 32 bits: what a small pool gives."""
+    rng = np.random.default_rng(16)
+    small, far = 41, 2_200_000
+    lens = [300, 33, 270]
+    table = np.stack((np.arange(19), np.arange(38, 57) % small, np.arange(19, 38))).astype(np.int32)
+    spread = np.concatenate((np.arange(0, 10), rng.permutation(np.arange(far - 200, far))[: small - 10])).astype(np.int32)
+    task, pos = np.repeat([0, 2], 40), np.concatenate((np.arange(260, 300), np.arange(230, 270)))
+    hq, hkv, d = 8, 2, 128  # K of 18 GB, bounds of 1.1 GB and then of 4.6 GB
+    k, v, q = normal(rng, 80, hkv, d), normal(rng, 80, hkv, d), normal(rng, 80, hq, d)
+    fill_k, fill_v = normal(rng, small, hkv, PAGE, d), normal(rng, small, hkv, PAGE, d)
+    results = []
+    for pages, at in ((small, np.arange(small, dtype=np.int32)), (far, spread)):
+        bt = at[table]
+        kv = tide.PagedKV(pages, hq, hkv, d, bt, fill_canary=False)
+        ids = dev(at, np.int64)
+        kv.k_pool[ids], kv.v_pool[ids] = fill_k, fill_v
+        bounds = kv.new_bounds()
+        kv.key_bounds(dev(lens), bounds)
+        slot = bt[task, pos // PAGE].astype(np.int64) * PAGE + pos % PAGE
+        kv.append_slots(k, v, dev(slot, np.int64), bounds)
+        sel = kv.select_blocks(q, dev(task), dev(pos), bounds, 5, 1, 1)
+        few = kv.select_blocks(q[[39, 79]], dev([0, 2]), dev([299, 269]), bounds, 5, 1, 1)
+        results.append([kv.k_pool[ids], kv.v_pool[ids], bounds[0][ids], bounds[1][ids], sel, few,
+                        kv.sparse(q, dev(task), dev(pos), sel), kv.sparse(q[[39, 79]], dev([0, 2]), dev([299, 269]), few)])
+        if pages == far:  # the bounds again, four times as far apart
+            wide = tide.PagedKV(1, hq, hkv, d, 4 * bt, fill_canary=False)
+            b = [torch.empty((4 * far,) + x.shape[1:], dtype=torch.int8, device="cuda") for x in bounds]
+            for x, y in zip(b, bounds):
+                x[4 * ids] = y[ids]
+            for rows, s in ((slice(None), sel), ([39, 79], few)):
+                assert torch.equal(wide.select_blocks(q[rows], dev(task[rows]), dev(pos[rows]), b, 5, 1, 1), s)
+            del wide, b
+        del kv, bounds
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_two_steps_at_once():
+    """Two engines on streams of their own, without a wait between them: what each gives alone."""
+    def make(seed):
+        rng = np.random.default_rng(seed)
+        return engine(2, 20, 40), [[normal(rng, e, x, D) for x in (HQ, HKV, HKV)] for e in (250, 2, 2, 60)]
+
+    wants = [[150, 100], [151, 101], [152, 102], [202, 112]]
+    alone, both = [], []
+    for seed in (17, 18):
+        (kv, table, bounds), args = make(seed)
+        alone.append([step(kv, table, dev(w), table.new_rows(a[0].shape[0]), *a, bounds) for w, a in zip(wants, args)])
+    engines = [make(17), make(18)]
+    w = [dev(x) for x in wants]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in engines]
+    both = [[], []]
+    for i in range(len(wants)):
+        for j, ((kv, table, bounds), args) in enumerate(engines):
+            with torch.cuda.stream(streams[j]):
+                both[j].append(step(kv, table, w[i], table.new_rows(args[i][0].shape[0]), *args[i], bounds))
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        for x, y in zip(a, b):
+            assert all(torch.equal(m, n) for m, n in zip(x, y))
 
 
 def test_bounds_after_other_appends():

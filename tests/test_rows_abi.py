@@ -75,6 +75,15 @@ def test_rows_of_nothing():
     assert call("tide_block_select", rows=0, budget=0) == tide.TIDE_ERR_INVALID_ARG
 
 
+def test_budget_limits():
+    for name in ("tide_block_select", "tide_sparse_attn"):
+        assert call(name, budget=2**30 + 1) == tide.TIDE_ERR_UNSUPPORTED
+    with pytest.raises(tide.TideError) as e:
+        tide.tide_rows_workspace_size(tide.TIDE_OP_SPARSE_ATTN, 1, GOOD, budget=2**30 + 1)
+    assert e.value.status == tide.TIDE_ERR_UNSUPPORTED
+    assert tide.tide_rows_workspace_size(tide.TIDE_OP_SPARSE_ATTN, 1, GOOD, budget=2**30) > 0
+
+
 def test_page_map_limits():
     assert call("tide_page_map", n=1 << 20, stride=1 << 11) == tide.TIDE_ERR_UNSUPPORTED
     assert call("tide_page_map", rows=2**31 - 1) == tide.TIDE_ERR_UNSUPPORTED
@@ -191,7 +200,7 @@ class TestBinding:
         assert tuple(b.shape) == (3, 2, 2, 64) and tuple(u.shape) == (3, 2) and b.dtype == u.dtype == torch.int8
 
 
-@pytest.mark.parametrize("src", ["page_map.hip", "key_bounds.hip", "block_select.hip", "sparse_attn.hip"])
+@pytest.mark.parametrize("src", ["page_map.hip", "key_bounds.hip", "block_select.hip", "sparse_attn.hip", "sparse_shared.hip"])
 def test_no_scratch_access_inside_loops(tmp_path, src):
     found = loops_with_scratch(_asm(tmp_path, src))
     assert found or src == "key_bounds.hip"
