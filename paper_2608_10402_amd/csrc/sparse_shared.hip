@@ -12,6 +12,7 @@
 // of rows taken together are looked at, and rows with one that is not finite are taken again, one by one; so are
 // rows that list a block twice, which a mark does not count.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_decode.h"
 
@@ -21,10 +22,11 @@ namespace kern {
 constexpr float kNoKeysYet = -3.0e38f;  // as kNoKeys of sparse_attn.hip
 constexpr int kSharedWaves = 4, kSharedThreads = kSharedWaves * 64;
 
-// The same number, which the compiler cannot see through: offsets made from it stay where they are used.  Kept from
-// one turn of the loop over tasks to the next they cost more registers than there are.
-__device__ __forceinline__ int unknown(int x) {
-  asm volatile("" : "+v"(x));
+// The lane, worked out where it is used: offsets made from a lane that is known from the start are kept from one turn
+// of the loop over tasks to the next, and cost more registers than there are.
+__device__ __forceinline__ int lane_now() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(x));
   return x;
 }
 
@@ -40,7 +42,7 @@ void sparse_shared_kernel(SparseArgs a) {
   using KL = KLds<D>;
   using VL = VLds<D>;
   constexpr int kC = D / 32, kT = D / 16, kWaves = kSharedWaves;
-  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, grp = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int Hkv = a.num_kv_heads, G = a.group, R = a.rows_at_once, shift = a.padded_shift;
   const int nth = blockIdx.x / Hkv, head = blockIdx.x - nth * Hkv;
@@ -90,7 +92,7 @@ void sparse_shared_kernel(SparseArgs a) {
 
     // ---- the packed list ----
     int entries;
-    const int me = unknown(tid);
+    const int me = 64 * wave + lane_now();
     if (me == 0) flags = 0;
     if (alone) {
       entries = a.budget;
@@ -137,7 +139,7 @@ void sparse_shared_kernel(SparseArgs a) {
         to += __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0)) << k;
         all += (uint32_t)__popcll(who) << k;
       }
-      if (lane == 0) sums[wave] = all;
+      if ((me & 63) == 0) sums[wave] = all;
       __syncthreads();
       entries = 0;
 #pragma unroll
@@ -161,18 +163,18 @@ void sparse_shared_kernel(SparseArgs a) {
     __syncthreads();
 
     // ---- its attention ----
-    const int l0 = unknown(lane);
+    const int l0 = lane_now(), col = l0 & 15, grp = l0 >> 4;
     uint32_t k_src[KL::kDma];
 #pragma unroll
     for (int i = 0; i < KL::kDma; ++i) k_src[i] = KL::src_offset(i, l0);
-    const uint32_t k_rd_even = KL::lds_offset(l0 & 15, l0 >> 4), k_rd_odd = KL::lds_offset(l0 & 15, 4 + (l0 >> 4));
+    const uint32_t k_rd_even = KL::lds_offset(col, grp), k_rd_odd = KL::lds_offset(col, 4 + grp);
     const uint32_t v_off = (uint32_t)(16 * l0);
     constexpr int kRpl = 1024 / (2 * D);
     uint32_t v_wr[DecodeRegs<D>::kLoads];
 #pragma unroll
     for (int i = 0; i < DecodeRegs<D>::kLoads; ++i)
       v_wr[i] = VL::offset(i * kRpl + l0 / VL::kNG, l0 % VL::kNG);
-    const int vr = 4 * (l0 >> 4) + ((l0 & 15) >> 2);
+    const int vr = 4 * grp + (col >> 2);
     // (of piece t: v_rd ^ 32 t, since a row's swizzle is an exclusive or of the same bits; registers are scarce here)
     const uint32_t v_rd = (uint32_t)(vr * 2 * D + 32 * VL::vsw(vr) + 8 * (l0 & 3));
     const int pairs = (entries + 1) / 2;
@@ -182,7 +184,7 @@ void sparse_shared_kernel(SparseArgs a) {
     uint64_t open = 0;
     auto fetch = [&]() {
       while (open == 0 && next_pair < pairs) {
-        const int at = 2 * (next_pair + kWaves * (lane >> 1)) + (lane & 1);
+        const int at = 2 * (next_pair + kWaves * (l0 >> 1)) + (l0 & 1);
         next_pair += 32 * kWaves;
         page = at < entries ? list_page[at] : -1;
         what = at < entries ? list_what[at] : 0;
@@ -224,7 +226,7 @@ void sparse_shared_kernel(SparseArgs a) {
       const int r = (16 * t + col) >> shift, h = (16 * t + col) & ((1 << shift) - 1);
       const bool on = h < G && r < R && (subset >> r) & 1;
       bit[t] = on ? 1u << r : 0;
-      pos_of[t] = __shfl(my_pos, r & 63, 64);
+      pos_of[t] = __builtin_amdgcn_ds_bpermute(4 * r, my_pos);
       const int first = (16 * t) >> shift, end = (16 * t + 15) >> shift;
       tile_rows[t] = subset & ((2u << min(end, 30)) - (1u << min(first, 30)));
       const int64_t at = ((row0 + (on ? r : r0)) * a.num_q_heads + head * G + (on ? h : 0)) * D;
@@ -249,7 +251,7 @@ void sparse_shared_kernel(SparseArgs a) {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < DecodeRegs<D>::kLoads; ++i)
-            if ((t ? p1 : p0) + i * kRpl + lane / VL::kNG > last) cur.v[t][i] = zero_u32x4();
+            if ((t ? p1 : p0) + i * kRpl + l0 / VL::kNG > last) cur.v[t][i] = zero_u32x4();
       }
       f32x4 s[kTiles][2];
 #pragma unroll
@@ -315,14 +317,31 @@ void sparse_shared_kernel(SparseArgs a) {
           }
         pb[u] = as_bf16x8(wp);
       }
+      // (one branch for all pieces of V: with one a product, each read was waited for by itself)
+      auto add_pv = [&](auto first, auto last) __attribute__((always_inline)) {
+        constexpr int kFirst = decltype(first)::value, kLast = decltype(last)::value;
+        constexpr int kAtOnce = 4;
 #pragma unroll
-      for (int t = 0; t < kT; ++t) {
-        const uint2 v0 = read_tr(vbuf + (v_rd ^ (32 * t))), v1 = read_tr(vbuf + KL::kPageBytes + (v_rd ^ (32 * t)));
-        const bf16x8 vv = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+        for (int t0 = 0; t0 < kT; t0 += kAtOnce) {
+          bf16x8 vv[kAtOnce];
 #pragma unroll
-        for (int u = 0; u < kTiles; ++u)
-          if (kTiles == 1 || (rows & tile_rows[u])) o[u][t] = mfma16(vv, pb[u], o[u][t]);
-      }
+          for (int t = 0; t < kAtOnce; ++t) {
+            const uint32_t at = v_rd ^ (32 * (t0 + t));
+            const uint2 v0 = read_tr(vbuf + at), v1 = read_tr(vbuf + KL::kPageBytes + at);
+            vv[t] = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
+          }
+#pragma unroll
+          for (int t = 0; t < kAtOnce; ++t)
+#pragma unroll
+            for (int u = kFirst; u <= kLast; ++u) o[u][t0 + t] = mfma16(vv[t], pb[u], o[u][t0 + t]);
+        }
+      };
+      constexpr std::integral_constant<int, 0> tile0;
+      constexpr std::integral_constant<int, kTiles - 1> tile1;
+      if (kTiles == 1) add_pv(tile0, tile0);
+      else if (!(rows & tile_rows[0])) add_pv(tile1, tile1);
+      else if (!(rows & tile_rows[kTiles - 1])) add_pv(tile0, tile0);
+      else add_pv(tile0, tile1);
     };
 
     {
@@ -349,7 +368,7 @@ void sparse_shared_kernel(SparseArgs a) {
       v += xor_shfl(v, 16);
       return v + xor_shfl(v, 32);
     };
-    const int l1 = unknown(lane), c1 = l1 & 15, g1 = l1 >> 4;
+    const int l1 = lane_now(), c1 = l1 & 15, g1 = l1 >> 4;
 #pragma unroll
     for (int u = 0; u < kTiles; ++u) {
       const float l = sum_cols(l_part[u]), lx = sum_cols(l_exact[u]);
@@ -360,7 +379,7 @@ void sparse_shared_kernel(SparseArgs a) {
       if (g1 == 0) stats[wave][16 * u + c1] = f32x4{m_ref[u], l, lx, 0.0f};
     }
     __syncthreads();
-    const int it = unknown(tid), il = it & 63;
+    const int it = 64 * wave + lane_now(), il = it & 63;
     // whether a row has a key at all: it lists a block of the pool (every listed block has one)
     uint32_t listed = 0, with_keys = 0;
     for (int i = il; i < entries; i += 64) listed |= list_page[i] >= 0 ? list_what[i] & 0xFF : 0u;
