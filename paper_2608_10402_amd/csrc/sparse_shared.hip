@@ -30,9 +30,20 @@ __device__ __forceinline__ int lane_now() {
   return x;
 }
 
-// An entry of the packed list: the block in the upper 24 bits, the rows that list it in the lower 8.
+// f over the four lane groups of 16, in every lane.
+template <class F>
+__device__ __forceinline__ float over_groups(float x, F&& f) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t y = __builtin_bit_cast(uint32_t, f(__builtin_bit_cast(float, (uint32_t)s[0]), __builtin_bit_cast(float, (uint32_t)s[1])));
+  const auto t = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  return f(__builtin_bit_cast(float, (uint32_t)t[0]), __builtin_bit_cast(float, (uint32_t)t[1]));
+}
+
+// An entry of the packed list: its page, and its block in the upper 24 bits of the other word, the rows that list it in
+// the lower 8 (none where there is no page to read).
 struct SharedStep {
-  int n0, n1;              // 1 where the step has the entry
+  bool there;
   uint32_t what0, what1;
 };
 
@@ -42,17 +53,16 @@ void sparse_shared_kernel(SparseArgs a) {
   using KL = KLds<D>;
   using VL = VLds<D>;
   constexpr int kC = D / 32, kT = D / 16, kWaves = kSharedWaves;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hkv = a.num_kv_heads, G = a.group, R = a.rows_at_once, shift = a.padded_shift;
   const int nth = blockIdx.x / Hkv, head = blockIdx.x - nth * Hkv;
   const int64_t row0 = (int64_t)a.first_row + (int64_t)nth * R;
   // K pages of the two steps in flight; marks before them, outputs after them
   __shared__ __attribute__((aligned(1024))) uint8_t k_lds0[kWaves * 2 * KL::kPageBytes];
   __shared__ __attribute__((aligned(1024))) uint8_t k_lds1[kWaves * 2 * KL::kPageBytes];
-  __shared__ int32_t list_page[kSharedEntries];
-  __shared__ uint32_t list_what[kSharedEntries];
+  __shared__ __attribute__((aligned(16))) uint2 list_of[kSharedEntries + 1];
   __shared__ f32x4 stats[kWaves][16 * kTiles];
+  __shared__ int32_t row_task[kSharedRows], row_pos[kSharedRows], used;
   __shared__ uint32_t sums[kWaves], flags;  // flags: rows that have to be taken again
   static_assert(sizeof(k_lds0) >= kSharedBlocks<D>, "a mark a block");
   uint8_t* const ka = k_lds0 + wave * 2 * KL::kPageBytes;
@@ -60,18 +70,31 @@ void sparse_shared_kernel(SparseArgs a) {
   uint32_t* const marks = reinterpret_cast<uint32_t*>(k_lds0);
   const uint8_t* kpool = reinterpret_cast<const uint8_t*>(a.k_pool);
   const uint8_t* vpool = reinterpret_cast<const uint8_t*>(a.v_pool);
+  constexpr uint32_t kMine = 2 * KL::kPageBytes;  // of a wave in either
   constexpr int64_t kBlk = (int64_t)kPage * D * 2;
 
-  // lane r: row r
-  int my_task = -1, my_pos = -1;
-  if (lane < R && (int64_t)nth * R + lane < a.rows) {
-    my_task = a.row_task[row0 + lane];
-    my_pos = a.row_pos[row0 + lane];
-    if (!live_row(my_task, my_pos, a.num_tasks, (int64_t)a.bt_stride * kPage)) my_task = -1;
+  // lane r: row r.  (In LDS, not in registers, while attention runs; every wave writes the same.)
+  auto load_rows = [&](int& task, int& pos) {
+    const int l = lane_now();
+    task = pos = -1;
+    if (l < R) task = row_task[l], pos = row_pos[l];
+  };
+  uint32_t left = 0, solo = 0;
+  {
+    const int l = lane_now();
+    int task = -1, pos = -1;
+    if (l < R && (int64_t)nth * R + l < a.rows) {
+      task = a.row_task[row0 + l];
+      pos = a.row_pos[row0 + l];
+      if (!live_row(task, pos, a.num_tasks, (int64_t)a.bt_stride * kPage)) task = -1;
+    }
+    if (l < R) row_task[l] = task, row_pos[l] = pos;
+    left = (uint32_t)__builtin_amdgcn_ballot_w64(task >= 0);
   }
-  uint32_t left = (uint32_t)__builtin_amdgcn_ballot_w64(my_task >= 0), solo = 0;
   bool flag_error = false;
   while (left) {
+    int my_task, my_pos;
+    load_rows(my_task, my_pos);
     const int r0 = __builtin_ctz(left), task = __builtin_amdgcn_readlane(my_task, r0);
     const uint32_t same = (uint32_t)__builtin_amdgcn_ballot_w64(my_task == task) & left & ~solo;
     const uint32_t subset = (solo >> r0) & 1 ? 1u << r0 : same;
@@ -83,26 +106,28 @@ void sparse_shared_kernel(SparseArgs a) {
       least = min(least, pos);
       last = max(last, pos);
     }
-    auto page_of = [&](int b) {
+    auto entry = [&](int b, uint32_t rows) {
       const int32_t page = table[b];
       const bool ok = page >= 0 && page < a.num_pages;
       flag_error |= !ok;
-      return ok ? page : -1;
+      return ok ? uint2{(uint32_t)page, (uint32_t)b << 8 | rows} : uint2{0u, 0u};
     };
 
     // ---- the packed list ----
     int entries;
     const int me = 64 * wave + lane_now();
-    if (me == 0) flags = 0;
+    if (me == 0) flags = 0, used = 0;
     if (alone) {
-      entries = a.budget;
       const int32_t* list = a.sel + ((row0 + r0) * Hkv + head) * a.budget;
-      for (int i = me; i < entries; i += kSharedThreads) {
+      __syncthreads();
+      for (int i = me; i < a.budget; i += kSharedThreads) {
         const int32_t b = list[i];
         const bool in = b >= 0 && b <= last / kPage;
-        list_page[i] = in ? page_of(b) : -1;
-        list_what[i] = (uint32_t)(in ? b : 0) << 8 | subset;
+        list_of[i] = in ? entry(b, subset) : uint2{0u, 0u};
+        if (in) atomicMax(&used, i + 1);
       }
+      __syncthreads();
+      entries = __builtin_amdgcn_readfirstlane(used);
     } else {
       const int words = (last / kPage + 4) / 4;
       for (int i = me; i < words; i += kSharedThreads) marks[i] = 0;
@@ -154,12 +179,12 @@ void sparse_shared_kernel(SparseArgs a) {
         for (int i = 0; i < 4; ++i) {
           const uint32_t rows = (m >> (8 * i)) & 0xFF;
           if (rows) {
-            list_page[to] = page_of(4 * w + i);
-            list_what[to++] = (uint32_t)(4 * w + i) << 8 | rows;
+            list_of[to++] = entry(4 * w + i, rows);
           }
         }
       }
     }
+    if (me == 0) list_of[entries] = uint2{0u, 0u};  // (the other of the last pair)
     __syncthreads();
 
     // ---- its attention ----
@@ -167,57 +192,37 @@ void sparse_shared_kernel(SparseArgs a) {
     uint32_t k_src[KL::kDma];
 #pragma unroll
     for (int i = 0; i < KL::kDma; ++i) k_src[i] = KL::src_offset(i, l0);
-    const uint32_t k_rd_even = KL::lds_offset(col, grp), k_rd_odd = KL::lds_offset(col, 4 + grp);
+    const uint32_t k_rd = kMine * wave + KL::lds_offset(col, grp);  // odd pieces: ^ 64
     const uint32_t v_off = (uint32_t)(16 * l0);
     constexpr int kRpl = 1024 / (2 * D);
-    uint32_t v_wr[DecodeRegs<D>::kLoads];
-#pragma unroll
-    for (int i = 0; i < DecodeRegs<D>::kLoads; ++i)
-      v_wr[i] = VL::offset(i * kRpl + l0 / VL::kNG, l0 % VL::kNG);
+    // (of load i: 1024 i + (v_wr ^ what i changes of the row's swizzle))
+    const uint32_t v_wr = kMine * wave + VL::offset(l0 / VL::kNG, l0 % VL::kNG);
+    auto v_place = [&](int i) { return (v_wr ^ (32u * VL::vsw(i * kRpl))) + 1024 * i; };
     const int vr = 4 * grp + (col >> 2);
     // (of piece t: v_rd ^ 32 t, since a row's swizzle is an exclusive or of the same bits; registers are scarce here)
-    const uint32_t v_rd = (uint32_t)(vr * 2 * D + 32 * VL::vsw(vr) + 8 * (l0 & 3));
+    const uint32_t v_rd = kMine * wave + (uint32_t)(vr * 2 * D + 32 * VL::vsw(vr) + 8 * (l0 & 3));
     const int pairs = (entries + 1) / 2;
     int next_pair = wave;
-    int32_t page = 0;
-    uint32_t what = 0;
-    uint64_t open = 0;
-    auto fetch = [&]() {
-      while (open == 0 && next_pair < pairs) {
-        const int at = 2 * (next_pair + kWaves * (l0 >> 1)) + (l0 & 1);
-        next_pair += 32 * kWaves;
-        page = at < entries ? list_page[at] : -1;
-        what = at < entries ? list_what[at] : 0;
-        open = __builtin_amdgcn_ballot_w64(page >= 0);
-      }
-    };
     auto issue = [&](DecodeRegs<D>& r, uint8_t* kbuf) {
-      fetch();
-      int64_t b0 = 0, b1 = 0;
-      SharedStep s = {0, 0, 0, 0};
-      if (open) {
-        const int i = __builtin_ctzll(open);
-        open &= open - 1;
-        s.n0 = 1;
-        s.what0 = (uint32_t)__builtin_amdgcn_readlane((int)what, i);
-        b0 = ((int64_t)__builtin_amdgcn_readlane(page, i) * Hkv + head) * kBlk;
+      SharedStep s = {next_pair < pairs, 0u, 0u};
+      uint32_t page0 = 0, page1 = 0;
+      if (s.there) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(&list_of[2 * next_pair]);
+        page0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[0]);
+        s.what0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[1]);
+        page1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[2]);
+        s.what1 = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[3]);
+        next_pair += kWaves;
       }
-      if (open) {
-        const int i = __builtin_ctzll(open);
-        open &= open - 1;
-        s.n1 = 1;
-        s.what1 = (uint32_t)__builtin_amdgcn_readlane((int)what, i);
-        b1 = ((int64_t)__builtin_amdgcn_readlane(page, i) * Hkv + head) * kBlk;
-      }
-      const int z0 = s.n0 ? (int)kBlk : 0, z1 = s.n1 ? (int)kBlk : 0;
+      const int64_t b0 = ((int64_t)page0 * Hkv + head) * kBlk, b1 = ((int64_t)page1 * Hkv + head) * kBlk;
+      const int z0 = (s.what0 & 0xFF) ? (int)kBlk : 0, z1 = (s.what1 & 0xFF) ? (int)kBlk : 0;
       load_step<D, kSharedPolicy>(r, kbuf, block_rsrc(kpool + b0, z0), block_rsrc(kpool + b1, z1),
                                   block_rsrc(vpool + b0, z0), block_rsrc(vpool + b1, z1), k_src, v_off);
       return s;
     };
 
     // column `col` of product t: row and head, its bit, its position
-    uint32_t bit[kTiles], tile_rows[kTiles];
-    int pos_of[kTiles];
+    uint32_t bit[kTiles];
     bf16x8 qf[kTiles][kC];
     f32x4 o[kTiles][kT];
     float m_ref[kTiles], l_part[kTiles], l_exact[kTiles];
@@ -226,9 +231,6 @@ void sparse_shared_kernel(SparseArgs a) {
       const int r = (16 * t + col) >> shift, h = (16 * t + col) & ((1 << shift) - 1);
       const bool on = h < G && r < R && (subset >> r) & 1;
       bit[t] = on ? 1u << r : 0;
-      pos_of[t] = __builtin_amdgcn_ds_bpermute(4 * r, my_pos);
-      const int first = (16 * t) >> shift, end = (16 * t + 15) >> shift;
-      tile_rows[t] = subset & ((2u << min(end, 30)) - (1u << min(first, 30)));
       const int64_t at = ((row0 + (on ? r : r0)) * a.num_q_heads + head * G + (on ? h : 0)) * D;
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
@@ -241,17 +243,17 @@ void sparse_shared_kernel(SparseArgs a) {
       l_part[t] = l_exact[t] = 0.0f;
     }
 
-    auto compute = [&](DecodeRegs<D>& cur, const uint8_t* kbuf, const SharedStep& st) {
+    auto compute = [&](DecodeRegs<D>& cur, uint8_t* lds, const SharedStep& st) {  // lds: k_lds0 or k_lds1
       const int p0 = (int)(st.what0 >> 8) * kPage, p1 = (int)(st.what1 >> 8) * kPage;  // first positions
-      const uint32_t rows = (st.what0 | st.what1) & 0xFF;
       const bool tail = max(p0, p1) + kPage - 1 > least;  // some key may be past some row's position
       if (tail) {
         // V rows past every position must not reach the MFMA (NaN * 0 = NaN)
+        const int l2 = lane_now();
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < DecodeRegs<D>::kLoads; ++i)
-            if ((t ? p1 : p0) + i * kRpl + l0 / VL::kNG > last) cur.v[t][i] = zero_u32x4();
+            if ((t ? p1 : p0) + i * kRpl + l2 / VL::kNG > last) cur.v[t][i] = zero_u32x4();
       }
       f32x4 s[kTiles][2];
 #pragma unroll
@@ -259,8 +261,7 @@ void sparse_shared_kernel(SparseArgs a) {
         u32x4 kk[kC];
 #pragma unroll
         for (int c = 0; c < kC; ++c)
-          kk[c] = *reinterpret_cast<const u32x4*>(kbuf + t * KL::kPageBytes + 1024 * (c >> 1) +
-                                                  ((c & 1) ? k_rd_odd : k_rd_even));
+          kk[c] = *reinterpret_cast<const u32x4*>(lds + (k_rd ^ (64 * (c & 1))) + t * KL::kPageBytes + 1024 * (c >> 1));
 #pragma unroll
         for (int u = 0; u < kTiles; ++u) {
           s[u][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -268,19 +269,19 @@ void sparse_shared_kernel(SparseArgs a) {
           for (int c = 0; c < kC; ++c) s[u][t] = mfma16(as_bf16x8(kk[c]), qf[u][c], s[u][t]);
         }
       }
-      uint8_t* vbuf = const_cast<uint8_t*>(kbuf);  // V over the K copy, which is done with
+      // V over the K copy, which is done with
 #pragma unroll
       for (int hp = 0; hp < 2; ++hp)
 #pragma unroll
         for (int i = 0; i < DecodeRegs<D>::kLoads; ++i)
-          *reinterpret_cast<u32x4*>(vbuf + hp * KL::kPageBytes + v_wr[i]) = cur.v[hp][i];
+          *reinterpret_cast<u32x4*>(lds + v_place(i) + hp * KL::kPageBytes) = cur.v[hp][i];
       bf16x8 pb[kTiles];
 #pragma unroll
       for (int u = 0; u < kTiles; ++u) {
-        if (kTiles > 1 && !(rows & tile_rows[u])) continue;  // no row of this product
-        const bool in0 = (st.what0 & bit[u]) != 0, in1 = st.n1 && (st.what1 & bit[u]) != 0;
+        const bool in0 = (st.what0 & bit[u]) != 0, in1 = (st.what1 & bit[u]) != 0;
         if (tail) {  // keys past the row's position
-          const int n0 = pos_of[u] - p0 + 1 - 4 * grp, n1 = pos_of[u] - p1 + 1 - 4 * grp;
+          const int l2 = lane_now(), r = (16 * u + (l2 & 15)) >> shift;
+          const int n0 = row_pos[min(r, kSharedRows - 1)] + 1 - 4 * (l2 >> 4) - p0, n1 = n0 + p0 - p1;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             s[u][0][e] = e < n0 ? s[u][0][e] : -INFINITY;
@@ -291,8 +292,7 @@ void sparse_shared_kernel(SparseArgs a) {
         const float top1 = fmaxf(fmaxf(s[u][1][0], s[u][1][1]), fmaxf(s[u][1][2], s[u][1][3]));
         float mt = a.scale_log2 * fmaxf(in0 ? top0 : -INFINITY, in1 ? top1 : -INFINITY);
         if (__any(mt > m_ref[u] + kRescaleSlack)) {  // only then is the column's maximum worked out
-          mt = fmaxf(mt, xor_shfl(mt, 16));
-          mt = fmaxf(mt, xor_shfl(mt, 32));
+          mt = over_groups(mt, [](float x, float y) { return fmaxf(x, y); });
           const float m_new = fmaxf(m_ref[u], mt);
           const float alpha = fast_exp2(m_ref[u] - m_new);
           l_part[u] *= alpha;
@@ -317,45 +317,35 @@ void sparse_shared_kernel(SparseArgs a) {
           }
         pb[u] = as_bf16x8(wp);
       }
-      // (one branch for all pieces of V: with one a product, each read was waited for by itself)
-      auto add_pv = [&](auto first, auto last) __attribute__((always_inline)) {
-        constexpr int kFirst = decltype(first)::value, kLast = decltype(last)::value;
-        constexpr int kAtOnce = 4;
+      constexpr int kAtOnce = 4;
 #pragma unroll
-        for (int t0 = 0; t0 < kT; t0 += kAtOnce) {
-          bf16x8 vv[kAtOnce];
+      for (int t0 = 0; t0 < kT; t0 += kAtOnce) {
+        bf16x8 vv[kAtOnce];
 #pragma unroll
-          for (int t = 0; t < kAtOnce; ++t) {
-            const uint32_t at = v_rd ^ (32 * (t0 + t));
-            const uint2 v0 = read_tr(vbuf + at), v1 = read_tr(vbuf + KL::kPageBytes + at);
-            vv[t] = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
-          }
-#pragma unroll
-          for (int t = 0; t < kAtOnce; ++t)
-#pragma unroll
-            for (int u = kFirst; u <= kLast; ++u) o[u][t0 + t] = mfma16(vv[t], pb[u], o[u][t0 + t]);
+        for (int t = 0; t < kAtOnce; ++t) {
+          const uint32_t at = v_rd ^ (32 * (t0 + t));
+          const uint2 v0 = read_tr(lds + at), v1 = read_tr(lds + at + KL::kPageBytes);
+          vv[t] = as_bf16x8(u32x4{v0.x, v0.y, v1.x, v1.y});
         }
-      };
-      constexpr std::integral_constant<int, 0> tile0;
-      constexpr std::integral_constant<int, kTiles - 1> tile1;
-      if (kTiles == 1) add_pv(tile0, tile0);
-      else if (!(rows & tile_rows[0])) add_pv(tile1, tile1);
-      else if (!(rows & tile_rows[kTiles - 1])) add_pv(tile0, tile0);
-      else add_pv(tile0, tile1);
+#pragma unroll
+        for (int t = 0; t < kAtOnce; ++t)
+#pragma unroll
+          for (int u = 0; u < kTiles; ++u) o[u][t0 + t] = mfma16(vv[t], pb[u], o[u][t0 + t]);
+      }
     };
 
     {
       DecodeRegs<D> ra, rb;
       SharedStep sa = issue(ra, ka), sb;
       // no wave reads marks any more, which the loads overwrite
-      while (sa.n0) {
+      while (sa.there) {
         sb = issue(rb, kb);
         __builtin_amdgcn_sched_barrier(0);
-        compute(ra, ka, sa);
-        if (!sb.n0) break;
+        compute(ra, k_lds0, sa);
+        if (!sb.there) break;
         sa = issue(ra, ka);
         __builtin_amdgcn_sched_barrier(0);
-        compute(rb, kb, sb);
+        compute(rb, k_lds1, sb);
       }
     }
 
@@ -364,14 +354,11 @@ void sparse_shared_kernel(SparseArgs a) {
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     __builtin_amdgcn_s_waitcnt(0);
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    auto sum_cols = [&](float v) {
-      v += xor_shfl(v, 16);
-      return v + xor_shfl(v, 32);
-    };
+    auto add = [](float x, float y) { return x + y; };
     const int l1 = lane_now(), c1 = l1 & 15, g1 = l1 >> 4;
 #pragma unroll
     for (int u = 0; u < kTiles; ++u) {
-      const float l = sum_cols(l_part[u]), lx = sum_cols(l_exact[u]);
+      const float l = over_groups(l_part[u], add), lx = over_groups(l_exact[u], add);
       uint8_t* to = u ? kb : ka;
 #pragma unroll
       for (int t = 0; t < kT; ++t)
@@ -382,15 +369,14 @@ void sparse_shared_kernel(SparseArgs a) {
     const int it = 64 * wave + lane_now(), il = it & 63;
     // whether a row has a key at all: it lists a block of the pool (every listed block has one)
     uint32_t listed = 0, with_keys = 0;
-    for (int i = il; i < entries; i += 64) listed |= list_page[i] >= 0 ? list_what[i] & 0xFF : 0u;
+    for (int i = il; i < entries; i += 64) listed |= list_of[i].y & 0xFF;
 #pragma unroll
     for (int r = 0; r < kSharedRows; ++r) with_keys |= __any((listed >> r) & 1) ? 1u << r : 0u;
     constexpr int kPiece = D / 4;  // 16-byte pieces of a head's output
     uint32_t again = 0;
-    for (int i = it; i < R * G * kPiece; i += kSharedThreads) {
-      const int rh = i / kPiece, p = i % kPiece, r = rh / G, h = rh - r * G;
-      if (!((subset >> r) & 1)) continue;
-      const int c = (r << shift) + h, j = c & 15;
+    for (int i = it; i < (R << shift) * kPiece; i += kSharedThreads) {
+      const int c = i / kPiece, p = i % kPiece, r = c >> shift, h = c & ((1 << shift) - 1), j = c & 15;
+      if (h >= G || !((subset >> r) & 1)) continue;
       const uint8_t* from = (c < 16 ? k_lds0 : k_lds1) + 4 * D * j + 16 * (p ^ j);
       f32x4 st[kWaves];
       float m = kNoKeysYet;
