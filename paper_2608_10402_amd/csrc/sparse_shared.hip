@@ -132,15 +132,20 @@ void sparse_shared_kernel(SparseArgs a) {
       const int words = (last / kPage + 4) / 4;
       for (int i = me; i < words; i += kSharedThreads) marks[i] = 0;
       __syncthreads();
-      for (int r = r0; r < R; ++r) {
+      for (int r = wave; r < R; r += kWaves) {  // a row a wave, four entries of a lane on their way
         if (!((subset >> r) & 1)) continue;
         const int blocks = __builtin_amdgcn_readlane(my_pos, r) / kPage + 1;
         const int32_t* list = a.sel + ((row0 + r) * Hkv + head) * a.budget;
-        for (int i = me; i < a.budget; i += kSharedThreads) {
-          const int32_t b = list[i];
-          if (b < 0 || b >= blocks) continue;
-          const uint32_t bit = 1u << (8 * (b & 3) + r);
-          if (atomicOr(&marks[b >> 2], bit) & bit) flags = 1u;  // (any thread that finds it writes the same)
+        for (int i = me & 63; i < a.budget; i += 256) {
+          int32_t b[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) b[u] = list[min(i + 64 * u, a.budget - 1)];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (i + 64 * u >= a.budget || b[u] < 0 || b[u] >= blocks) continue;
+            const uint32_t bit = 1u << (8 * (b[u] & 3) + r);
+            if (atomicOr(&marks[b[u] >> 2], bit) & bit) flags = 1u;  // (any thread that finds it writes the same)
+          }
         }
       }
       __syncthreads();
@@ -178,11 +183,11 @@ void sparse_shared_kernel(SparseArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t rows = (m >> (8 * i)) & 0xFF;
-          if (rows) {
-            list_of[to++] = entry(4 * w + i, rows);
-          }
+          if (rows) list_of[to++] = uint2{(uint32_t)(4 * w + i), rows};
         }
       }
+      __syncthreads();
+      for (int i = me; i < entries; i += kSharedThreads) list_of[i] = entry((int)list_of[i].x, list_of[i].y);
     }
     if (me == 0) list_of[entries] = uint2{0u, 0u};  // (the other of the last pair)
     __syncthreads();
