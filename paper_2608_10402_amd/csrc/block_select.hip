@@ -231,6 +231,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t score_rsrc(const BlockSelectAr
 // chunk come U F0 F1 F2.  So what is issued behind F0 before its step is at least F1 F2 U P F3 (later chunks have
 // stores between them); behind F1, F2 U P F3 S0 F0; behind F2, U P F3 S0 F0 S1 F1; behind F3, S0 F0 S1 F1 S2 F2;
 // behind U and P before the next chunk begins, F0 F1 F2.  The order of an S and the F beside it is free.
+// (256 rows of 8 heads, contexts of 1k-32k: 117 us with 4 waves a workgroup, 131 with 8, 120 with 2.)
 constexpr int kRowWaves = 4;
 
 // The operands of one step, read once all but kWait of the wave's vector-memory operations are done.
@@ -865,8 +866,9 @@ int select_tile_rows(int32_t group, bool chunk) {
   return chunk ? kern::kChunkTiles * (16 >> kern::padded_shift(group)) : 1;
 }
 
-// Up to this many (row, kv head) pairs take four waves each, more one each.
-constexpr uint32_t kChooseWide = 512;
+// Up to this many (row, kv head) pairs take four waves each, more one each (scores and choice of rows of 8 heads, contexts
+// of 4k-16k, four waves and one: 16 rows 15.7 and 17.1 us, 128 rows 48.0 and 49.5, 256 rows 85.1 and 83.0).
+constexpr uint32_t kChooseWide = 1024;
 
 hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, hipStream_t stream) {
   // (a context within the budget has nothing to choose: no scores are read)

@@ -25,7 +25,8 @@ namespace kern {
 typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBoundWaves = 4;
-constexpr int64_t kAppendWaves = 16384;
+constexpr int64_t kAppendWaves = 8192;
+constexpr int32_t kAppendWindow = 4;
 
 // One page's rows as its wave loads them: lane l has piece l % kG of rows l / kG + kRows i.
 template <int D>
@@ -134,7 +135,7 @@ __device__ __forceinline__ void put_bounds(const PageRows<D>& rows, int8_t* boun
   if (lane == 0) units[at] = (int8_t)(finite ? unit : kNoUnit);
 }
 
-// A workgroup looks at a.window rows (1 or 16) for the first rows of pages.  Such a row, with those behind it that
+// A workgroup looks at a.window rows (1 or kAppendWindow) for the first rows of pages.  Such a row, with those behind it that
 // follow in the same page, is an item for each kv head, and the items go round the workgroups of the window
 // (gridDim.y) and their waves.
 template <int D, bool kBounds>
@@ -191,7 +192,8 @@ __global__ __launch_bounds__(kBoundWaves * 64) void slot_append_kernel(SlotAppen
   }
 }
 
-// One wave per (task, kBoundPages pages, kv head): all of them in flight at once.
+// One wave per (task, kBoundPages pages, kv head): all of them in flight at once, read past the caches (687 MB of keys:
+// 144 us with ordinary loads, 130 without; 125 with two entries an instruction, 5.5 TB/s).
 constexpr int kBoundPages = 4;
 
 template <int D>
@@ -239,10 +241,12 @@ __global__ __launch_bounds__(kBoundWaves * 64) void key_bounds_kernel(KeyBoundsA
 template <int D>
 hipError_t append_slots(const SlotAppendArgs& args, hipStream_t stream) {
   SlotAppendArgs a = args;
-  // Few rows: a workgroup for 4 kv heads of each, so that the call ends soon.  More than the device holds waves:
-  // one for 16 rows, since 15 of 16 rows of an observation are not the first of a page, and a wave that only finds
-  // that out costs a third of one that works (35,144 rows of 4 heads: a wave a row and head 47 us, a wave a row 35).
-  a.window = (int64_t)a.num_rows * a.num_kv_heads > kAppendWaves ? kPage : 1;
+  // Few rows: a workgroup for 4 kv heads of each, so that the call ends soon.  More than the device holds waves: one for
+  // 4 rows, since 15 of 16 rows of an observation are not the first of a page, and a wave that only finds that out
+  // costs a third of one that works; single tokens, which all are, want short windows.  (A call by windows of 1, 4 and
+  // 16 rows: 64 x 512 rows of 4 heads 36, 24 and 24 us; 16 x 512 of 8 heads 22, 14, 14; 1,024 x 1 of 8 heads 9, 11, 33;
+  // 4,096 x 1 of 8 heads 25, 20, 37.)
+  a.window = (int64_t)a.num_rows * a.num_kv_heads > kAppendWaves ? kAppendWindow : 1;
   const uint32_t parts = a.window > 1 ? 1 : (uint32_t)((a.num_kv_heads + kBoundWaves - 1) / kBoundWaves);
   // a launch holds fewer than 2^32 threads
   const int32_t most = (int32_t)((1 << 23) / parts) * a.window;

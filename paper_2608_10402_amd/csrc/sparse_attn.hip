@@ -6,12 +6,16 @@
 // so a row costs its list and not its context, and neither the length nor the position has to be known
 // to the host.
 //
-// One workgroup takes a (row, kv head), or a part of its list where there are few (splits): wave w of W
-// takes the pairs of entries w, w + W, ...: 32 keys a step, the G heads as MFMA columns.  Its lanes hold
+// One workgroup takes a (row, kv head), or a part of its list where there are few (splits): wave w of 4
+// takes the pairs of entries w, w + 4, ...: 32 keys a step, the G heads as MFMA columns.  Its lanes hold
 // the page ids of 64 entries at a time and entries that name nothing (negative, beyond the row's
 // position, a page id out of range) are left out of them, so a step always has a page to read.  The step
 // is that of the decode kernels (K through LDS, V transposed in LDS; attn_decode.h), with the next step
 // in flight while one is used.  The waves' parts are joined in LDS, in wave order.
+//
+// A decode batch reads its lists' pages once and is bound by HBM: 256 rows of 128 blocks (32 / 8 heads, d = 128), 2.1 GB
+// in 315 us, 6.7 TB/s.  Few rows are bound by the chain list entry, page id, K and V, join: 4 rows of 64 blocks
+// (28 / 4 heads) 11.1 us.
 #include <algorithm>
 
 #include "attn_decode.h"
@@ -23,10 +27,11 @@ namespace kern {
 // score but -inf.
 constexpr float kNoKeys = -3.0e38f;
 
-// Waves of a workgroup: 8 where its workgroups leave CUs idle (kWide), 4 else.
-constexpr int kSparseWide = 8, kSparseWaves = 4;
+// Waves of a workgroup.  (8 for calls that leave CUs idle: 4 rows of 64 blocks 10.7 us instead of 11.1, 16 rows of 256
+// 30.6 instead of 29.7.)
+constexpr int kWaves = 4;
 
-template <int D, int kPolicy, int kWaves>
+template <int D, int kPolicy>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void sparse_attn_kernel(SparseArgs a) {
   using KL = KLds<D>;
@@ -306,10 +311,7 @@ __global__ __launch_bounds__(256) void sparse_merge_kernel(SparseArgs a) {
 template <int D, int kPolicy>
 void launch_lists(const SparseArgs& a, hipStream_t stream) {
   const uint32_t groups = (uint32_t)a.rows * (uint32_t)a.num_kv_heads * (uint32_t)a.splits;
-  if (groups <= kSparseAlone)
-    hipLaunchKernelGGL((sparse_attn_kernel<D, kPolicy, kSparseWide>), dim3(groups), dim3(kSparseWide * 64), 0, stream, a);
-  else
-    hipLaunchKernelGGL((sparse_attn_kernel<D, kPolicy, kSparseWaves>), dim3(groups), dim3(kSparseWaves * 64), 0, stream, a);
+  hipLaunchKernelGGL((sparse_attn_kernel<D, kPolicy>), dim3(groups), dim3(kWaves * 64), 0, stream, a);
 }
 
 template <int D>
@@ -324,14 +326,10 @@ hipError_t launch_sparse_d(const SparseArgs& a, bool shared, hipStream_t stream)
 }
 
 // Every variant is instantiated explicitly (see attn_decode.hip).
-template __global__ void sparse_attn_kernel<128, kSharedPolicy, kSparseWide>(SparseArgs);
-template __global__ void sparse_attn_kernel<128, kSharedPolicy, kSparseWaves>(SparseArgs);
-template __global__ void sparse_attn_kernel<128, kStreamPolicy, kSparseWide>(SparseArgs);
-template __global__ void sparse_attn_kernel<128, kStreamPolicy, kSparseWaves>(SparseArgs);
-template __global__ void sparse_attn_kernel<64, kSharedPolicy, kSparseWide>(SparseArgs);
-template __global__ void sparse_attn_kernel<64, kSharedPolicy, kSparseWaves>(SparseArgs);
-template __global__ void sparse_attn_kernel<64, kStreamPolicy, kSparseWide>(SparseArgs);
-template __global__ void sparse_attn_kernel<64, kStreamPolicy, kSparseWaves>(SparseArgs);
+template __global__ void sparse_attn_kernel<128, kSharedPolicy>(SparseArgs);
+template __global__ void sparse_attn_kernel<128, kStreamPolicy>(SparseArgs);
+template __global__ void sparse_attn_kernel<64, kSharedPolicy>(SparseArgs);
+template __global__ void sparse_attn_kernel<64, kStreamPolicy>(SparseArgs);
 
 }  // namespace kern
 

@@ -596,7 +596,7 @@ constexpr int kSharedEntries = 1536, kSharedRows = 8;
 template <int D>
 constexpr int kSharedBlocks = 8 * kPage * D * 2;
 
-// Workgroups of a call up to which each has a CU of its own, and takes 8 waves.
+// Workgroups of a call up to which each has a CU of its own.
 constexpr uint32_t kSparseAlone = 256;
 
 struct SparseArgs {

@@ -393,6 +393,21 @@ def test_choice_in_rounds():
     c.check(c.queries(n), task, np.array([c.rng.integers(300, c.lens[b]) for b in task]), 10, 1, 1)
 
 
+def test_choice_of_many_tasks_with_a_few_rows_each():
+    """Enough rows that workgroups walk several tasks, in rounds too."""
+    rng = np.random.default_rng(19)
+    lens = list(rng.integers(60, 400, 260))
+    c = Choice(19, lens, 8, 2, 64)
+    task = np.repeat(np.arange(260), 4)
+    c.check(c.queries(task.size), task, np.array([rng.integers(50, lens[b]) for b in task]), 7, 1, 1)
+    wide = np.full((260, 1 << 15), 2**31 - 1, np.int32)  # 256 KB of scores a row: rounds of 1,024 rows
+    wide[:, :c.table.shape[1]] = c.table
+    c.table = wide
+    c.kv.set_block_table(wide)
+    assert tide.tide_rows_workspace_size(tide.TIDE_OP_BLOCK_SELECT, task.size, c.kv.dims, max_len=1 << 19) == (256 << 20) + 256
+    c.check(c.queries(task.size), task, np.array([rng.integers(50, lens[b]) for b in task]), 7, 0, 2)
+
+
 # ---- attention over lists -----------------------------------------------------------------------------
 
 class Sparse:
@@ -590,6 +605,22 @@ def test_large_scores_and_values():
     s.p.k[...] = -np.abs(s.p.k)
     s.upload()
     s.check(np.abs(q), task, pos, np.tile(np.arange(50), (6, 1, 1)))
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 128), (16, 2, 64)])
+def test_large_scores_of_rows_taken_together(hq, hkv, d):
+    """The same for rows of one task, whose lists differ, so that their maxima rise at different blocks."""
+    s = Sparse(7, [1600], hq, hkv, d, scale=20.0)
+    s.p.k *= (2.0 ** (np.arange(s.p.k.shape[0]) % 4))[:, None, None, None]
+    s.upload()
+    q, task, pos = s.rows(600)
+    pos[:] = 1000 + np.arange(600)
+    sel = s.lists(task, pos, 30)
+    sel[:, :, 0] = pos[:, None] // PAGE
+    for r in range(600):  # (distinct blocks, the last one first)
+        for h in range(hkv):
+            sel[r, h, 1:][sel[r, h, 1:] == sel[r, h, 0]] = -1
+    s.check(q, task, pos, sel, only=range(0, 600, 7))
 
 
 def test_keys_that_are_not_numbers_reach_the_rows_that_list_them():
