@@ -74,15 +74,17 @@ SelectRounds select_rounds(int32_t num_rows, int32_t max_len, const tide_dims& d
   return r;
 }
 
-// ---- sparse attention: workgroups that share a (row, kv head) where there are few of them.  A part keeps 16
-// steps for each of its waves: less does not pay for the second kernel, which joins the parts (4 rows of 64 blocks and
-// 4 kv heads: 6.4 + 4 us in four parts, 11.1 in one, and a launch less).
-constexpr int32_t kLeastPairs = 64;
+// ---- sparse attention: workgroups that share a (row, kv head) where there are few of them.  A part keeps 4 steps for
+// each of its 4 waves, and there are none where the whole has fewer than 12: less does not pay for the second kernel,
+// which joins the parts.  (4 rows of 4 kv heads: 64 blocks 12.4 us in one part, 15.2 in two; 128 blocks 22.0 in one,
+// 16.7 in two, 14.6 in four; 256 blocks 40.1 in one, 26.1 in two, 15.2 in eight.)
+constexpr int32_t kLeastPairs = 16, kSplitPairs = 48;
 constexpr int32_t kSparseLaunch = 1 << 23; // workgroups of a launch (fewer than 2^32 threads)
 
 int32_t sparse_splits(int64_t num_rows, int32_t budget, const tide_dims& dims) {
   const int64_t units = num_rows * dims.num_kv_heads;
   const int64_t pairs = ((int64_t)budget + 1) / 2;
+  if (pairs < kSplitPairs) return 1;
   return (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSparseAlone / units, pairs / kLeastPairs));
 }
 
