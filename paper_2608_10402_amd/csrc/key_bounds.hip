@@ -25,8 +25,6 @@ namespace kern {
 typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBoundWaves = 4;
-constexpr int64_t kAppendWaves = 8192;
-constexpr int32_t kAppendWindow = 4;
 
 // One page's rows as its wave loads them: lane l has piece l % kG of rows l / kG + kRows i.
 template <int D>
@@ -135,7 +133,7 @@ __device__ __forceinline__ void put_bounds(const PageRows<D>& rows, int8_t* boun
   if (lane == 0) units[at] = (int8_t)(finite ? unit : kNoUnit);
 }
 
-// A workgroup looks at a.window rows (1 or kAppendWindow) for the first rows of pages.  Such a row, with those behind it that
+// A workgroup looks at a.window rows (append_window) for the first rows of pages.  Such a row, with those behind it that
 // follow in the same page, is an item for each kv head, and the items go round the workgroups of the window
 // (gridDim.y) and their waves.
 template <int D, bool kBounds>
@@ -238,15 +236,18 @@ __global__ __launch_bounds__(kBoundWaves * 64) void key_bounds_kernel(KeyBoundsA
     if (at[i] >= 0) put_bounds<D>(k[i], a.bounds, a.units, at[i]);
 }
 
+// Few (row, kv head) pairs: a workgroup for 4 kv heads of each row, so that the call ends soon.  More than the device
+// holds waves: one for several rows, since 15 of 16 rows of an observation are not the first of a page, and a wave that
+// only finds that out costs a third of one that works; single tokens, which all are, want short windows.  (A call by
+// windows of 1, 4, 8 and 16 rows: 1,024 x 1 rows of 8 heads 9.3, 10.9, 18.6 and 33 us; 4,096 x 1 of 8 heads 25, 20, 25,
+// 37; 8,192 x 1 of 8 heads 46, 38, 38, 49; 64 x 512 of 4 heads 36, 24, 24, 24; 64 x 64-2,048 of 4 heads by the last three
+// 38, 35, 34; 64 x 1,024 of 8 heads 195, 118, 118, 119.)
+int32_t append_window(int64_t pairs) { return pairs <= 8192 ? 1 : pairs < 65536 ? 4 : 8; }
+
 template <int D>
 hipError_t append_slots(const SlotAppendArgs& args, hipStream_t stream) {
   SlotAppendArgs a = args;
-  // Few rows: a workgroup for 4 kv heads of each, so that the call ends soon.  More than the device holds waves: one for
-  // 4 rows, since 15 of 16 rows of an observation are not the first of a page, and a wave that only finds that out
-  // costs a third of one that works; single tokens, which all are, want short windows.  (A call by windows of 1, 4 and
-  // 16 rows: 64 x 512 rows of 4 heads 36, 24 and 24 us; 16 x 512 of 8 heads 22, 14, 14; 1,024 x 1 of 8 heads 9, 11, 33;
-  // 4,096 x 1 of 8 heads 25, 20, 37.)
-  a.window = (int64_t)a.num_rows * a.num_kv_heads > kAppendWaves ? kAppendWindow : 1;
+  a.window = append_window((int64_t)a.num_rows * a.num_kv_heads);
   const uint32_t parts = a.window > 1 ? 1 : (uint32_t)((a.num_kv_heads + kBoundWaves - 1) / kBoundWaves);
   // a launch holds fewer than 2^32 threads
   const int32_t most = (int32_t)((1 << 23) / parts) * a.window;

@@ -149,8 +149,10 @@ def rows_of(prefix, extend):
 APPEND = [  # prefix, extend, kv heads, d
     ([0], [1], 1, 64), ([15], [1], 2, 128), ([3, 0, 40], [5, 33, 0], 4, 128), ([7, 16, 31], [60, 16, 2], 5, 64),
     ([1000], [129], 3, 128), ([0] * 40, [17] * 40, 1, 128), (list(range(33)), [1] * 33, 8, 128), ([14], [4], 64, 64),
-    # more rows x kv heads than are taken one by one: windows of 16 rows, few and many first rows of pages in each
-    ([5, 100], [210, 61], 64, 64), (list(range(70, 370)), [1] * 300, 64, 64), ([3] * 37, [7] * 37, 65, 128)]
+    # more rows x kv heads than are taken one by one: windows of rows, few and many first rows of pages in each
+    ([5, 100], [210, 61], 64, 64), (list(range(70, 370)), [1] * 300, 64, 64), ([3] * 37, [7] * 37, 65, 128),
+    # and longer windows
+    ([5, 100], [700, 401], 64, 64), ([i % 17 for i in range(340)], [1 + i % 5 for i in range(340)], 65, 64)]
 
 
 @pytest.mark.parametrize("prefix,extend,hkv,d", APPEND)
