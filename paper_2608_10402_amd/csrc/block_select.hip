@@ -552,7 +552,7 @@ constexpr int kChooseSame = 64;    // scores of one bin that are ranked against 
 constexpr int kNoScore = INT32_MIN;  // in the place of a block that is not to be chosen from
 
 template <int kT>
-constexpr int kChooseHeld = kT == 64 ? 16 : 8;  // quads that a thread holds: contexts of 65,536 or 131,072
+constexpr int kChooseHeld = kT == 128 ? 12 : 8;  // quads that a thread holds: contexts of 98,304 or 131,072
 
 __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {  // inclusive
   const int lane = threadIdx.x & 63;
@@ -694,14 +694,12 @@ __global__ __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(4))) void ch
 #pragma unroll
     for (int i = 0; i < kChooseWords / kT; ++i) bits[tid + i * kT] = 0;
     if (tid == 0) sames = quads = 0;
-    if (kWaves > 1 && lane == 0) extreme[0][wave] = low, extreme[1][wave] = high;
+    if (lane == 0) extreme[0][wave] = low, extreme[1][wave] = high;
     __syncthreads();
-    if (kWaves > 1) {
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        low = min(low, extreme[0][w]);
-        high = max(high, extreme[1][w]);
-      }
+    for (int w = 0; w < kWaves; ++w) {
+      low = min(low, extreme[0][w]);
+      high = max(high, extreme[1][w]);
     }
     if (low > score_order(-INFINITY) && high < score_order(INFINITY)) {
       int least = low;
@@ -717,21 +715,17 @@ __global__ __launch_bounds__(kT) __attribute__((amdgpu_waves_per_eu(4))) void ch
         clear_bins();
       }
       // the quads that reach it
-      int listed = 0;
       each4([&](const i32x4& x, int p) {
         const bool in = max4(x) >= least;
         const uint64_t who = __builtin_amdgcn_ballot_w64(in);
-        int base = listed;
-        if (kWaves > 1) {
-          if (lane == 0) base = atomicAdd(&quads, (int)__popcll(who));
-          base = __builtin_amdgcn_readfirstlane(base);
-        }
+        int base = 0;
+        if (lane == 0) base = atomicAdd(&quads, (int)__popcll(who));
+        base = __builtin_amdgcn_readfirstlane(base);
         const int to = base + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
         if (in && to < kChooseQuads) quad[to] = x, quad_at[to] = p;
-        listed += (int)__popcll(who);
       });
       __syncthreads();
-      if (kWaves > 1) listed = quads;
+      const int listed = quads;
       if (listed <= kChooseQuads) {
         const ScoreBins bin(least, high);
         const int* key_of = reinterpret_cast<const int*>(quad);
@@ -866,8 +860,9 @@ int select_tile_rows(int32_t group, bool chunk) {
   return chunk ? kern::kChunkTiles * (16 >> kern::padded_shift(group)) : 1;
 }
 
-// Up to this many (row, kv head) pairs take four waves each, more one each (scores and choice of rows of 8 heads, contexts
-// of 4k-16k, four waves and one: 16 rows 15.7 and 17.1 us, 128 rows 48.0 and 49.5, 256 rows 85.1 and 83.0).
+// Up to this many (row, kv head) pairs take four waves each, more two: 16 pairs, contexts of 2k-16k, 5.6 us with four
+// waves, 7.2 with two, 9.5 with one; 14,000 pairs, contexts of 32k-98k, 175, 78 and 86 us; calls of 1,024 pairs, scores and
+// choice, 48.4 and 48.5 us with four and two, of 2,048 pairs 85.6 and 82.3.
 constexpr uint32_t kChooseWide = 1024;
 
 hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, hipStream_t stream) {
@@ -878,7 +873,7 @@ hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, hipStream
   if (rc != hipSuccess) return rc;
   const uint32_t pairs = (uint32_t)(a.rows * a.num_kv_heads);
   if (pairs > kChooseWide)
-    hipLaunchKernelGGL((kern::choose_kernel<64>), dim3(pairs), dim3(64), 0, stream, a);
+    hipLaunchKernelGGL((kern::choose_kernel<128>), dim3(pairs), dim3(128), 0, stream, a);
   else
     hipLaunchKernelGGL((kern::choose_kernel<256>), dim3(pairs), dim3(256), 0, stream, a);
   return hipGetLastError();
