@@ -12,6 +12,10 @@
 // One workgroup scans the tasks, 2,048 a round, and then writes pages and rows element by element: each
 // finds its task by bisection of the sums in LDS, so one long task costs no more than many short ones.
 // Above kRowsHere rows a second kernel writes the rows from the results of the first.
+//
+// Latencies bound it: lengths, three scans with a barrier each, free pages, rows.  175 tasks of one token each take 7.2 us;
+// 1,056 tasks of 1-450 tokens, a tenth of which end (17,000 page ids go through one CU), 19 us, and their 69,946 rows
+// 4.8: 24 us a call, 32 with one task a thread and one element at a time.
 #include <type_traits>
 
 #include "kernels.h"
