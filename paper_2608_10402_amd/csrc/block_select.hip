@@ -391,7 +391,7 @@ void score_rows_kernel(BlockSelectArgs a) {
 // Several rows of most tasks: a workgroup takes the tile_rows rows of each of its waves, task by task (mostly one), and
 // all of its waves use the chunk of 64 blocks that they bring into LDS together, the next one on its way.  A kv
 // head's workgroups run on the same dies (workgroup b on die b % 8) where the number of kv heads lets them.
-// Vector instructions bound it (49% of SIMD cycles, products 32%): 1,761 rows of 64 / 8 heads over 8 contexts of 32k-98k
+// Vector instructions (41% of SIMD cycles) and products (27%) bound it, while long tasks' workgroups last longest: 1,761 rows of 64 / 8 heads over 8 contexts of 32k-98k
 // in 167 + 54 us, two rounds.  (302 us a call with the choice; 1,053 when each wave read operands of its own straight
 // from memory and choices were made by the general way.)
 constexpr int kChunkWaves = 4;

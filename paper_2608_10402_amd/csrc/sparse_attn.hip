@@ -14,8 +14,8 @@
 // in flight while one is used.  The waves' parts are joined in LDS, in wave order.
 //
 // A decode batch reads its lists' pages once and is bound by HBM: 256 rows of 128 blocks (32 / 8 heads, d = 128), 2.1 GB
-// in 315 us, 6.7 TB/s.  Few rows are bound by the chain list entry, page id, K and V, join: 4 rows of 64 blocks
-// (28 / 4 heads) 11.1 us.
+// in 320 us, 6.6 TB/s.  Few rows are bound by the chain list entry, page id, K and V, join: 4 rows of 64 blocks
+// (28 / 4 heads) 11 us.
 #include <algorithm>
 
 #include "attn_decode.h"

@@ -7,7 +7,7 @@
 // every K and V operand.  A column takes part where its row's mark is set and the key is not past its position.
 // Its traffic is the union of the lists, not their sum: 1,761 rows of 128 blocks each over 8 contexts of 32k-98k
 // (64 / 8 heads, d = 128), whose fours list 227-263 different blocks, take 675 us by single rows, which is what the L1s
-// deliver (16 KB a step of 32 keys), and 420 here (15 TB/s out of L2, 91% hits; registers and LDS hold two waves a
+// deliver (16 KB a step of 32 keys), and 410 here (16 TB/s out of L2, 91% hits; registers and LDS hold two waves a
 // SIMD).  Leaving out a product whose rows list neither block costs more than it saves: branches between products made
 // the accumulators be copied and each read of V be waited for by itself (470 us).
 //
