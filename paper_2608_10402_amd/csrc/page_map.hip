@@ -11,11 +11,12 @@
 //
 // One workgroup scans the tasks, 2,048 a round, and then writes pages and rows element by element: each
 // finds its task by bisection of the sums in LDS, so one long task costs no more than many short ones.
-// Above kRowsHere rows a second kernel writes the rows from the results of the first.
+// Above kRowsHere rows a second kernel writes the rows from the results of the first, and pages that go back to a large
+// table are moved by a kernel before it, whose workgroups scan all lengths again.
 //
 // Latencies bound it: lengths, three scans with a barrier each, free pages, rows.  175 tasks of one token each take 7.2 us;
-// 1,056 tasks of 1-450 tokens, a tenth of which end (17,000 page ids go through one CU), 19 us, and their 69,946 rows
-// 4.8: 24 us a call, 32 with one task a thread and one element at a time.
+// 1,056 tasks of 1-450 tokens, a tenth of which end, take 23 us a call with their 69,946 rows: 24 with the 17,000 page ids
+// through one CU, 32 with one task a thread and one element at a time.
 #include <type_traits>
 
 #include "kernels.h"
@@ -90,59 +91,51 @@ __device__ __forceinline__ void put_row(const PageMapArgs& a, int64_t r, int32_t
   a.row_slot[r] = slot;
 }
 
-__global__ __launch_bounds__(kMapThreads) void page_map_kernel(PageMapArgs a) {
-  __shared__ uint32_t tmp[4][kMapThreads / 64];
-  __shared__ uint32_t first_page[kMapTasks], first_row[kMapTasks];
-  __shared__ int32_t len_of[kMapTasks], want_of[kMapTasks];  // want: that of the call, or the length where refused
-  __shared__ uint32_t used;
-  const int tid = threadIdx.x;
-  const uint32_t count = (uint32_t)min(max(*a.free_count, 0), a.capacity);
+// Lengths of a thread's two neighbouring tasks of a round, from task b on; one whose lengths are no lengths stays as
+// it is.
+__device__ __forceinline__ void load_lengths(const PageMapArgs& a, int b, int32_t (&len)[2], int32_t (&want)[2]) {
   const int64_t most = (int64_t)a.bt_stride * kPage;
-  if (tid == 0) used = 0;
-
-  // a thread's two neighbouring tasks of a round; one whose lengths are no lengths stays as it is
-  int32_t len[2], want[2];
-  auto load = [&](int b) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      len[c] = want[c] = 0;
-      if (b + c >= a.num_tasks) continue;
-      len[c] = a.lens[b + c];
-      want[c] = a.want[b + c];
-      if (len[c] < 0 || len[c] > most || want[c] < 0 || want[c] > most) want[c] = len[c];
-    }
-  };
-  // sums of x over the tasks before each of a thread's two
-  auto sums_before = [&](const uint32_t (&x)[2], uint32_t* scratch, uint32_t (&before)[2], uint32_t* all) {
-    const uint32_t both = sat_add(x[0], x[1]), upto = map_scan(both, scratch, all);
-    before[0] = upto - both;  // (callers whose sums may be cut off use the sums up to a task instead)
-    before[1] = sat_add(before[0], x[0]);
-    return upto;
-  };
+  for (int c = 0; c < 2; ++c) {
+    len[c] = want[c] = 0;
+    if (b + c >= a.num_tasks) continue;
+    len[c] = a.lens[b + c];
+    want[c] = a.want[b + c];
+    if (len[c] < 0 || len[c] > most || want[c] < 0 || want[c] > most) want[c] = len[c];
+  }
+}
 
-  // f(how many elements of `all` a thread takes at once)
-  auto by_width = [](uint32_t all, auto&& f) {
-    if (all > kMapThreads) f(std::integral_constant<int, kMany>());
-    else f(std::integral_constant<int, 1>());
-  };
+// f(how many elements of `all` a thread takes at once)
+template <class F>
+__device__ __forceinline__ void by_width(uint32_t all, F&& f) {
+  if (all > kMapThreads) f(std::integral_constant<int, kMany>());
+  else f(std::integral_constant<int, 1>());
+}
 
-  // pages that go back, on top of the stack
-  const bool one_round = a.num_tasks <= kMapTasks;
+// Pages that go back, on top of a stack of `count`; returns how many.  Workgroup `part` of `parts` moves every parts-th
+// run of them (none: part < 0).  first_page, keep: LDS, a word a task of a round; tmp: as map_scan's; len, want: of the
+// last round on return.
+__device__ __forceinline__ uint32_t give_back(const PageMapArgs& a, uint32_t count, int part, int parts, uint32_t* first_page,
+                                              int32_t* keep, uint32_t* tmp, int32_t (&len)[2], int32_t (&want)[2]) {
+  const int tid = threadIdx.x;
   uint32_t back = 0;
   for (int t0 = 0; t0 < a.num_tasks; t0 += kMapTasks) {
-    load(t0 + 2 * tid);
-    uint32_t n[2], before[2], all;
+    load_lengths(a, t0 + 2 * tid, len, want);
+    uint32_t n[2], all;
 #pragma unroll
     for (int c = 0; c < 2; ++c) n[c] = want[c] < len[c] ? (uint32_t)(pages_of(len[c]) - pages_of(want[c])) : 0u;
-    sums_before(n, tmp[0], before, &all);  // (a table has fewer than 2^31 entries, so these sums are exact)
-    if (all > 0) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) first_page[2 * tid + c] = before[c], len_of[2 * tid + c] = want[c];
+    // (a table has fewer than 2^31 entries, so these sums are exact)
+    const uint32_t before = map_scan(n[0] + n[1], tmp, &all) - (n[0] + n[1]);
+    if (all > 0 && part >= 0) {
+      first_page[2 * tid] = before;
+      first_page[2 * tid + 1] = before + n[0];
+      keep[2 * tid] = want[0];
+      keep[2 * tid + 1] = want[1];
       __syncthreads();
       const int tasks = min(kMapTasks, a.num_tasks - t0);
-      auto give_back = [&](auto at_once) {
+      by_width(all, [&](auto at_once) {
         constexpr int kAtOnce = decltype(at_once)::value;
-        for (uint32_t j0 = tid; j0 < all; j0 += kAtOnce * kMapThreads) {
+        for (uint32_t j0 = tid + part * kAtOnce * kMapThreads; j0 < all; j0 += parts * kAtOnce * kMapThreads) {
           uint32_t j[kAtOnce];
           int i[kAtOnce];
           int32_t page[kAtOnce];
@@ -151,7 +144,7 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(PageMapArgs a) {
           last_at_most(first_page, tasks, j, i);
 #pragma unroll
           for (int u = 0; u < kAtOnce; ++u)
-            page[u] = a.block_table[(int64_t)(t0 + i[u]) * a.bt_stride + pages_of(len_of[i[u]]) +
+            page[u] = a.block_table[(int64_t)(t0 + i[u]) * a.bt_stride + pages_of(keep[i[u]]) +
                                     (int32_t)(j[u] - first_page[i[u]])];
 #pragma unroll
           for (int u = 0; u < kAtOnce; ++u) {
@@ -159,19 +152,51 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(PageMapArgs a) {
             if (j0 + u * kMapThreads < all && at < (uint32_t)a.capacity) a.free_pages[at] = page[u];
           }
         }
-      };
-      by_width(all, give_back);
-      back = sat_add(back, all);
+      });
     }
+    back = sat_add(back, all);
     __syncthreads();
   }
+  return back;
+}
+
+__device__ __forceinline__ uint32_t free_now(const PageMapArgs& a) { return (uint32_t)min(max(*a.free_count, 0), a.capacity); }
+
+// The pages that go back alone, by many workgroups, each of which scans all lengths.
+__global__ __launch_bounds__(kMapThreads) void give_back_kernel(PageMapArgs a) {
+  __shared__ uint32_t tmp[kMapThreads / 64], first_page[kMapTasks];
+  __shared__ int32_t keep[kMapTasks];
+  int32_t len[2], want[2];
+  give_back(a, free_now(a), blockIdx.x, gridDim.x, first_page, keep, tmp, len, want);
+}
+
+__global__ __launch_bounds__(kMapThreads) void page_map_kernel(PageMapArgs a) {
+  __shared__ uint32_t tmp[4][kMapThreads / 64];
+  __shared__ uint32_t first_page[kMapTasks], first_row[kMapTasks];
+  __shared__ int32_t len_of[kMapTasks], want_of[kMapTasks];  // want: that of the call, or the length where refused
+  __shared__ uint32_t used;
+  const int tid = threadIdx.x;
+  const uint32_t count = free_now(a);
+  if (tid == 0) used = 0;
+
+  int32_t len[2], want[2];
+  // sums of x over the tasks before each of a thread's two
+  auto sums_before = [&](const uint32_t (&x)[2], uint32_t* scratch, uint32_t (&before)[2], uint32_t* all) {
+    const uint32_t both = sat_add(x[0], x[1]), upto = map_scan(both, scratch, all);
+    before[0] = upto - both;  // (callers whose sums may be cut off use the sums up to a task instead)
+    before[1] = sat_add(before[0], x[0]);
+    return upto;
+  };
+
+  const bool one_round = a.num_tasks <= kMapTasks;
+  const uint32_t back = give_back(a, count, a.returns_apart ? -1 : 0, 1, first_page, len_of, tmp[0], len, want);
   const uint32_t there = min(sat_add(count, back), (uint32_t)a.capacity);
 
   // rows and pages of the tasks that grow
   uint32_t asked = 0, rows = 0, pages = 0;
   for (int t0 = 0; t0 < a.num_tasks; t0 += kMapTasks) {
     const int b = t0 + 2 * tid, tasks = min(kMapTasks, a.num_tasks - t0);
-    if (!one_round) load(b);
+    if (!one_round) load_lengths(a, b, len, want);
     uint32_t e[2], p[2], in_r[2], in_p[2], all_e, all_r, all_p;
 #pragma unroll
     for (int c = 0; c < 2; ++c) e[c] = want[c] > len[c] ? (uint32_t)(want[c] - len[c]) : 0u;
@@ -304,6 +329,12 @@ __global__ __launch_bounds__(kRowThreads) void map_rows_kernel(PageMapArgs a) {
 
 }  // namespace kern
 
+// Tables of this many entries have their returned pages moved by workgroups of their own, before the others: 2.8 us more
+// where none return (1,056 tasks of 4k-8k: 13.4 and 16.2 us), less where some do (a tenth of 4k-8k 33 and 19, four tenths
+// 95 and 16; a tenth of 16k-32k 92 and 19, four tenths 362 and 19).
+constexpr int64_t kTableHere = 1 << 16;
+constexpr uint32_t kReturnGroups = 128;
+
 // One workgroup writes this many rows itself (256 tasks of 16, 32 and 64 rows each: 14.7, 17.3 and 22.9 us by it alone,
 // 16.1 us each with the second kernel).
 constexpr int32_t kRowsHere = 4096;
@@ -311,6 +342,9 @@ constexpr int32_t kRowsHere = 4096;
 hipError_t launch_page_map(const PageMapArgs& args, hipStream_t stream) {
   PageMapArgs a = args;
   a.rows_apart = a.num_rows > kRowsHere;
+  a.returns_apart = (int64_t)a.num_tasks * a.bt_stride >= kTableHere;
+  if (a.returns_apart)
+    hipLaunchKernelGGL(kern::give_back_kernel, dim3(kReturnGroups), dim3(kern::kMapThreads), 0, stream, a);
   hipLaunchKernelGGL(kern::page_map_kernel, dim3(1), dim3(kern::kMapThreads), 0, stream, a);
   hipError_t rc = hipGetLastError();
   if (rc != hipSuccess || !a.rows_apart) return rc;

@@ -526,6 +526,7 @@ struct PageMapArgs {
   int32_t* row_pos;
   int64_t* row_slot;
   bool rows_apart;     // the rows are written by a kernel of their own
+  bool returns_apart;  // and the pages that go back are moved by one
 };
 
 // Key bounds: per (page, kv head) d upper and d lower bounds in whole units 2^units (kNoUnit: a key

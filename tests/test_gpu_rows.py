@@ -88,6 +88,19 @@ def test_page_map_of_long_tasks():
     same_map(want, lens, np.arange(n * stride).reshape(n, stride), np.zeros(n * stride, int), 0, 50)
 
 
+@pytest.mark.parametrize("n,pages,room", [(3, 190000, 10**6), (2500, 260, 10**6), (2100, 300, 50000), (1, 600000, 10**6)])
+def test_page_map_of_large_tables(n, pages, room):
+    """Tables whose returned pages are moved by workgroups of their own, some past the stack's end; in place too."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, PAGE * pages + 1, n)
+    want = np.where(rng.random(n) < 0.6, rng.integers(0, lens + 1), np.minimum(lens + rng.integers(0, 40, n), PAGE * pages))
+    want[0], lens[-1] = 0, PAGE * pages
+    table = rng.integers(0, 2**31 - 1, (n, pages))
+    free = rng.integers(0, 2**31 - 1, min(room, 10 + W.pages_of(lens.max()) * n))
+    for in_place in (False, True):
+        same_map(lens, want, table, free, 10, 3000, in_place=in_place)
+
+
 def test_page_map_keeps_the_stack_in_its_array():
     """Pages that do not fit are dropped; a count out of range is taken as the nearest that is not."""
     table = np.arange(30).reshape(3, 10)
