@@ -503,6 +503,8 @@ TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, 
  *   lens_out         int32 [num_tasks], may be lens itself; free_count_out may be free_count
  *   row_start        int32 [num_tasks + 1]: the first row of each task
  *   row_*            [num_rows]: the new tokens' rows, in task order; padding (-1) behind them
+ * Otherwise no array that is written may overlap another (TIDE_ERR_INVALID_ARG): lens_out is not want_lens, unless
+ * both are lens.
  * First every task with want < lens gives its pages from ceil(want / 16) on back, in task order and from
  * the first of them on (what does not fit in free_capacity is dropped).  Then, in task order, a task
  * with want > lens gets want - lens rows and ceil(want / 16) - ceil(lens / 16) pages from the top of the

@@ -28,6 +28,35 @@ int begin(const tide_dims* dims, int32_t count, int64_t num_pages, bool* go) {
   return TIDE_OK;
 }
 
+// Whether the arrays that a page map writes overlap another of its arrays.  One workgroup writes while others still read,
+// and rows are written from what was granted before: a refused task's length in the place of the wanted one would pass
+// for a granted one, with rows in pages that it was not given.  lens_out may be lens itself (a task's length is replaced
+// by the thread that read it, after its last use), also where lens is what is wanted, and free_count_out free_count.
+bool arrays_overlap(const PageMapArgs& a) {
+  struct Span {
+    uintptr_t at;
+    int64_t bytes;
+  };
+  auto span = [](const void* p, int64_t bytes) { return Span{reinterpret_cast<uintptr_t>(p), bytes}; };
+  const int64_t tasks = 4 * (int64_t)a.num_tasks, rows = 4 * (int64_t)a.num_rows;
+  const Span all[] = {span(a.lens, tasks), span(a.want, tasks), span(a.free_count, 4),
+                      // written:
+                      span(a.lens_out, tasks), span(a.free_count_out, 4),
+                      span(a.block_table, tasks * a.bt_stride), span(a.free_pages, 4 * (int64_t)a.capacity),
+                      span(a.row_start, tasks + 4), span(a.row_task, rows), span(a.row_pos, rows),
+                      span(a.row_slot, 2 * rows)};
+  constexpr int kRead = 3, kAll = sizeof(all) / sizeof(all[0]);
+  for (int j = kRead; j < kAll; ++j)
+    for (int i = 0; i < j; ++i) {
+      const Span &x = all[i], &y = all[j];
+      if (x.bytes == 0 || y.bytes == 0 || x.at >= y.at + y.bytes || y.at >= x.at + x.bytes) continue;
+      const bool lens = j == 3 && i < 2 && x.at == y.at && all[0].at == y.at;
+      const bool count = i == 2 && j == 4 && x.at == y.at;
+      if (!lens && !count) return true;
+    }
+  return false;
+}
+
 // The longest context of a call: max_len, or (0) all that the block table holds.
 int longest(int32_t max_len, int32_t bt_stride, int32_t* out) {
   const int64_t most = std::min<int64_t>((int64_t)bt_stride * kPage, INT32_MAX);
@@ -180,6 +209,7 @@ TIDE_API int tide_page_map(const int32_t* lens, const int32_t* want_lens, int32_
     a.row_task = row_task;
     a.row_pos = row_pos;
     a.row_slot = row_slot;
+    if (arrays_overlap(a)) return TIDE_ERR_INVALID_ARG;
     return launch_page_map(a, static_cast<hipStream_t>(stream)) == hipSuccess ? TIDE_OK : TIDE_ERR_HIP;
   } catch (...) {
     return TIDE_ERR_HIP;
