@@ -491,10 +491,15 @@ TIDE_API int tide_kv4_evict(void* kv4_pool, float* mass_pool, int64_t num_pages,
  *                entry, units = s; a page with a key that is not finite has unit 127 and zeros
  *
  * Workspace: tide_rows_workspace_size; num_rows, budget and max_len as the call gets them (budget: attention;
- * max_len: selection, the longest context, > 0).  It holds nothing between calls.
+ * max_len: selection, the longest context, > 0).  It holds nothing between calls.  Sizes are not monotone:
+ * the lists of fewer rows are split into more parts, and a round of selection holds whole rows.  A
+ * caller that keeps one workspace for batches that change takes tide_rows_workspace_bound for the most rows,
+ * the largest budget and the longest context: enough for every call within them.
  */
 TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, int32_t max_len,
                              const tide_dims* dims, size_t* bytes_out);
+TIDE_API int tide_rows_workspace_bound(int op, int32_t num_rows, int32_t budget, int32_t max_len,
+                              const tide_dims* dims, size_t* bytes_out);
 
 /*
  * Block tables and slot maps from lengths on the device.  All arrays are device memory.

@@ -23,7 +23,7 @@ from ._lib import (TIDE_ERR_CAPACITY, TIDE_ERR_HIP, TIDE_ERR_INVALID_ARG, TIDE_E
                    tide_kv4_decode_attn, tide_kv4_evict, tide_kv4_extend_attn, tide_kv4_unpack,
                    tide_kv_evict, TIDE_OP_BLOCK_SELECT, TIDE_OP_KEY_BOUNDS, TIDE_OP_SLOT_APPEND,
                    TIDE_OP_SPARSE_ATTN, tide_block_select, tide_key_bounds, tide_page_map,
-                   tide_rows_workspace_size, tide_slot_append, tide_sparse_attn)
+                   tide_rows_workspace_bound, tide_rows_workspace_size, tide_slot_append, tide_sparse_attn)
 from .kvcache import PagedKV, PagedKV4, PageTable
 
 __all__ = ["TIDE_ERR_CAPACITY", "TIDE_ERR_HIP", "TIDE_ERR_INVALID_ARG", "TIDE_ERR_PAGE_RANGE",
@@ -39,5 +39,5 @@ __all__ = ["TIDE_ERR_CAPACITY", "TIDE_ERR_HIP", "TIDE_ERR_INVALID_ARG", "TIDE_ER
            "tide_kv4_decode_append_attn", "tide_kv4_decode_attn", "tide_kv4_evict",
            "tide_kv4_extend_attn", "tide_kv4_unpack", "tide_kv_evict", "PageTable",
            "TIDE_OP_BLOCK_SELECT", "TIDE_OP_KEY_BOUNDS", "TIDE_OP_SLOT_APPEND", "TIDE_OP_SPARSE_ATTN",
-           "tide_block_select", "tide_key_bounds", "tide_page_map", "tide_rows_workspace_size",
+           "tide_block_select", "tide_key_bounds", "tide_page_map", "tide_rows_workspace_bound", "tide_rows_workspace_size",
            "tide_slot_append", "tide_sparse_attn"]

@@ -46,7 +46,7 @@ EXPORTED = ("tide_workspace_size", "tide_kv_append", "tide_extend_attn", "tide_d
             "tide_kv4_append", "tide_kv4_unpack", "tide_kv4_decode_attn",
             "tide_kv4_decode_append_attn", "tide_kv4_extend_attn", "tide_attn_mass",
             "tide_kv4_attn_mass", "tide_kv_evict", "tide_kv4_evict",
-            "tide_rows_workspace_size", "tide_page_map", "tide_slot_append", "tide_key_bounds",
+            "tide_rows_workspace_size", "tide_rows_workspace_bound", "tide_page_map", "tide_slot_append", "tide_key_bounds",
             "tide_block_select", "tide_sparse_attn",
             "tide_plan_info_get", "tide_ctb_create", "tide_ctb_step", "tide_ctb_get_stats", "tide_ctb_destroy",
             "tide_status_string", "tide_shutdown")
@@ -123,6 +123,7 @@ def load(path: str = LIB_PATH):
     lib.tide_kv4_evict.argtypes = [vp, vp, i64, vp, i32, vp, i32, i32, vp, vp, vp, dims_p, vp, vp,
                                    sz, vp]
     lib.tide_rows_workspace_size.argtypes = [ctypes.c_int, i32, i32, i32, dims_p, ctypes.POINTER(sz)]
+    lib.tide_rows_workspace_bound.argtypes = lib.tide_rows_workspace_size.argtypes
     lib.tide_page_map.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, dims_p,
                                   vp]
     lib.tide_slot_append.argtypes = [vp, vp, vp, i32, vp, vp, i64, vp, vp, dims_p, vp, sz, vp]
@@ -713,11 +714,20 @@ def tide_kv4_evict(kv4_pool, mass, block_table, kv_lens, keep_lens, dims: tide_d
 
 
 # ---- steps whose rows, lengths and block lists are device data -------------------------------------
-def tide_rows_workspace_size(op: int, num_rows: int, dims: tide_dims, budget: int = 0, max_len: int = 0) -> int:
+def _rows_workspace(name, op, num_rows, dims, budget, max_len):
     out = ctypes.c_size_t(0)
-    _check(load().tide_rows_workspace_size(op, int(num_rows), int(budget), int(max_len), ctypes.byref(dims),
-                                           ctypes.byref(out)), "tide_rows_workspace_size")
+    _check(getattr(load(), name)(op, int(num_rows), int(budget), int(max_len), ctypes.byref(dims), ctypes.byref(out)),
+           name)
     return int(out.value)
+
+
+def tide_rows_workspace_size(op: int, num_rows: int, dims: tide_dims, budget: int = 0, max_len: int = 0) -> int:
+    return _rows_workspace("tide_rows_workspace_size", op, num_rows, dims, budget, max_len)
+
+
+def tide_rows_workspace_bound(op: int, num_rows: int, dims: tide_dims, budget: int = 0, max_len: int = 0) -> int:
+    """Enough for every call with at most these rows, this budget and this longest context."""
+    return _rows_workspace("tide_rows_workspace_bound", op, num_rows, dims, budget, max_len)
 
 
 # A step of these calls is a few microseconds of GPU time, so what passes is checked in one look at each tensor.

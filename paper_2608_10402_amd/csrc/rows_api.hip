@@ -92,15 +92,27 @@ struct SelectRounds {
   size_t bytes;
 };
 
+int32_t score_stride(int32_t max_len) {
+  const int64_t blocks = ((int64_t)max_len + kPage - 1) / kPage;
+  return (int32_t)((blocks + kScoreChunk - 1) / kScoreChunk * kScoreChunk);
+}
+
 SelectRounds select_rounds(int32_t num_rows, int32_t max_len, const tide_dims& dims) {
   SelectRounds r;
-  const int64_t blocks = ((int64_t)max_len + kPage - 1) / kPage;
-  r.stride = (int32_t)((blocks + kScoreChunk - 1) / kScoreChunk * kScoreChunk);
+  r.stride = score_stride(max_len);
   const int64_t row = (int64_t)r.stride * dims.num_kv_heads * 4;
   const int64_t most = std::min<int64_t>(kScoreBytes / row, kRoundPairs / dims.num_kv_heads);
   r.rows = (int32_t)std::min<int64_t>(num_rows, std::max<int64_t>(1, most));
   r.bytes = kHeader + (size_t)((int64_t)r.rows * row);
   return r;
+}
+
+// At least select_rounds(n, m).bytes for every n <= num_rows and m <= max_len.  (Those fall where a row grows by so much that
+// one fewer fits in a round.)
+size_t select_bound(int32_t num_rows, int32_t max_len, const tide_dims& dims) {
+  const int64_t row = (int64_t)score_stride(max_len) * dims.num_kv_heads * 4;
+  if (row >= kScoreBytes) return kHeader + (size_t)row;
+  return kHeader + (size_t)std::min<int64_t>(kScoreBytes, num_rows * row);
 }
 
 // ---- sparse attention: workgroups that share a (row, kv head) where there are few of them.  A part keeps 4 steps for
@@ -125,6 +137,16 @@ size_t sparse_bytes(int32_t num_rows, int32_t budget, const tide_dims& dims, siz
   return *ml_off + rows * 16;
 }
 
+// At least sparse_bytes(n, b) for every n <= num_rows and b <= budget.  (Those fall where rows become so many that they are
+// split into fewer parts or none: a (row, kv head) has at most pairs / kLeastPairs parts, and all have at most kSparseAlone.)
+size_t sparse_bound(int32_t num_rows, int32_t budget, const tide_dims& dims) {
+  const int64_t pairs = ((int64_t)budget + 1) / 2;
+  if (pairs < kSplitPairs) return kHeader;
+  const int64_t most = kSparseAlone;  // (each factor is cut there before they are multiplied)
+  const int64_t units = std::min(most, (int64_t)num_rows * dims.num_kv_heads), parts = std::min(most, pairs / kLeastPairs);
+  return kHeader + (size_t)(std::min(most, units * parts) * (dims.num_q_heads / dims.num_kv_heads) * (dims.head_dim * 4 + 16));
+}
+
 // Up to this many (row, kv head) pairs rows are taken one by one even where they share a task: a workgroup each, all at
 // once (28 / 4 heads, 128 blocks, 64 rows of a task: 18 us, 31 together; 8 x 16 rows 31 and 35; 8 x 64 rows 103 and 52;
 // 32 / 8 heads, 8 x 16 rows: 55 and 40).
@@ -143,15 +165,9 @@ void shared_rows(int32_t num_rows, int32_t num_tasks, int32_t budget, int32_t bt
   *rows = std::max(1, std::min({kSharedRows, 32 >> *shift, kSharedEntries / budget}));
 }
 
-}  // namespace
-}  // namespace tide
-
-using namespace tide;
-
-extern "C" {
-
-TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, int32_t max_len, const tide_dims* dims,
-                                      size_t* bytes_out) {
+// bound: of every call with at most these rows, budget and longest context; else of this one.
+int rows_workspace(int op, int32_t num_rows, int32_t budget, int32_t max_len, const tide_dims* dims, bool bound,
+                   size_t* bytes_out) {
   try {
     const int rc = check_dims(dims);
     if (rc != TIDE_OK) return rc;
@@ -164,12 +180,16 @@ TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, 
         return TIDE_OK;
       case TIDE_OP_BLOCK_SELECT:
         if (max_len <= 0) return TIDE_ERR_INVALID_ARG;
-        *bytes_out = num_rows ? select_rounds(num_rows, max_len, *dims).bytes : kHeader;
+        *bytes_out = kHeader;
+        if (num_rows > 0)
+          *bytes_out = bound ? select_bound(num_rows, max_len, *dims) : select_rounds(num_rows, max_len, *dims).bytes;
         return TIDE_OK;
       case TIDE_OP_SPARSE_ATTN:
         if (budget <= 0) return TIDE_ERR_INVALID_ARG;
         if (budget > kMostBudget) return TIDE_ERR_UNSUPPORTED;
-        *bytes_out = num_rows ? sparse_bytes(num_rows, budget, *dims, &ml_off) : kHeader;
+        *bytes_out = kHeader;
+        if (num_rows > 0)
+          *bytes_out = bound ? sparse_bound(num_rows, budget, *dims) : sparse_bytes(num_rows, budget, *dims, &ml_off);
         return TIDE_OK;
       default:
         return TIDE_ERR_INVALID_ARG;
@@ -177,6 +197,23 @@ TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, 
   } catch (...) {
     return TIDE_ERR_HIP;
   }
+}
+
+}  // namespace
+}  // namespace tide
+
+using namespace tide;
+
+extern "C" {
+
+TIDE_API int tide_rows_workspace_size(int op, int32_t num_rows, int32_t budget, int32_t max_len, const tide_dims* dims,
+                                      size_t* bytes_out) {
+  return rows_workspace(op, num_rows, budget, max_len, dims, false, bytes_out);
+}
+
+TIDE_API int tide_rows_workspace_bound(int op, int32_t num_rows, int32_t budget, int32_t max_len, const tide_dims* dims,
+                                       size_t* bytes_out) {
+  return rows_workspace(op, num_rows, budget, max_len, dims, true, bytes_out);
 }
 
 TIDE_API int tide_page_map(const int32_t* lens, const int32_t* want_lens, int32_t num_tasks, int32_t* block_table,

@@ -81,6 +81,7 @@ class PagedKV(_Paged):
                  block_table, sm_scale: float | None = None, device="cuda",
                  fill_canary: bool = True):
         super().__init__(num_q_heads, num_kv_heads, head_dim, block_table, sm_scale, device)
+        self._rows_ws, self._rows_replaced, self._rows_fit = None, [], {}
         shape_k = shape_v = (num_pages, num_kv_heads, 16, head_dim)
         if fill_canary:
             self.k_pool = torch.full(shape_k, CANARY_BITS, dtype=torch.int16,
@@ -190,9 +191,26 @@ class PagedKV(_Paged):
                            keep_lens, recent_lens, new_block_table, kept, stream)
 
 
-    # ---- steps whose rows, lengths and block lists are device data.  A call that is captured into a
-    # graph keeps this object's workspace, which a later, larger call replaces: give a graph a PagedKV of
-    # its own over the same pools, or make its calls once before the capture and no larger ones after.
+    # ---- steps whose rows, lengths and block lists are device data.  They have a workspace of their own.  A graph goes on
+    # using the one that it was captured with, so one that a larger call replaces lives as long as this object.  What is
+    # in flight at once (a replay, and a call on another stream) takes a PagedKV each over the same pools.
+
+    def _rows_workspace(self, op, rows, longest=0):
+        """A workspace for a call of `op` with this many rows and this budget or longest context, and for every
+        smaller one."""
+        fit = self._rows_fit.get(op, (-1, 0))
+        if rows > fit[0] or longest > fit[1]:
+            fit = max(rows, fit[0]), max(longest, fit[1])
+            need = _lib.tide_rows_workspace_bound(op, fit[0], self.dims, budget=fit[1], max_len=fit[1])
+            old = self._rows_ws
+            if old is None or old.numel() < need:
+                # (at least twice the last: all that were replaced take less than the present one)
+                size = max(need, 1 << 16 if old is None else 2 * old.numel())
+                self._rows_ws = _lib.alloc_workspace(size, self.device)
+                if old is not None:
+                    self._rows_replaced.append(old)
+            self._rows_fit[op] = fit
+        return self._rows_ws
 
     def new_bounds(self):
         """Key bounds for append_slots, key_bounds and select_blocks: (bounds, units) of every page."""
@@ -204,15 +222,14 @@ class PagedKV(_Paged):
         """Store the rows' K/V in their slots (tide_slot_append); with bounds, bring those of the
         pages that change up to date."""
         b, u = bounds if bounds is not None else (None, None)
-        # (the smallest workspace there is holds the error flags, which is all these two calls need)
         _lib.tide_slot_append(k_new, v_new, row_slot, self.k_pool, self.v_pool, self.dims, b, u,
-                              self._ws if self._ws is not None else self.workspace(0), stream)
+                              self._rows_workspace(_lib.TIDE_OP_SLOT_APPEND, 0), stream)
 
     def key_bounds(self, lens, bounds, from_lens=None, max_len: int = 0, stream=None):
         """Key bounds of the pages that hold positions from_lens (None: 0) .. lens - 1 of each task, both on
         the device (tide_key_bounds): after append, extend_append, evict and what else writes keys."""
         _lib.tide_key_bounds(self.k_pool, self.block_table, lens, bounds[0], bounds[1], self.dims, from_lens, max_len,
-                             self._ws if self._ws is not None else self.workspace(0), stream)
+                             self._rows_workspace(_lib.TIDE_OP_KEY_BOUNDS, 0), stream)
         return bounds
 
     def select_blocks(self, q, row_task, row_pos, bounds, budget: int, sink: int = 0, recent: int = 0,
@@ -221,21 +238,20 @@ class PagedKV(_Paged):
         [rows][Hkv][budget]; those of padding rows are not written."""
         if out is None:
             out = torch.empty((q.shape[0], self.dims.num_kv_heads, budget), dtype=torch.int32, device=q.device)
-        longest = max_len if max_len > 0 else min(self.block_table.shape[1] * self.dims.page_size, 2**31 - 1)
-        self._call(lambda: _lib.tide_rows_workspace_size(_lib.TIDE_OP_BLOCK_SELECT, q.shape[0], self.dims,
-                                                         max_len=longest),
-                   lambda ws: _lib.tide_block_select(q, row_task, row_pos, bounds[0], bounds[1], self.block_table,
-                                                     budget, self.dims, out, sink, recent, max_len, ws, stream))
+        longest = min(self.block_table.shape[1] * self.dims.page_size, 2**31 - 1)
+        longest = min(max_len, longest) if max_len > 0 else longest
+        ws = self._rows_workspace(_lib.TIDE_OP_BLOCK_SELECT, q.shape[0], longest)
+        _lib.tide_block_select(q, row_task, row_pos, bounds[0], bounds[1], self.block_table, budget, self.dims, out,
+                               sink, recent, max_len, ws, stream)
         return out
 
     def sparse(self, q, row_task, row_pos, sel, out=None, lse=None, stream=None):
         """Attention of each row over the blocks in sel (tide_sparse_attn); padding rows are not
         written."""
         out = torch.empty_like(q) if out is None else out
-        self._call(lambda: _lib.tide_rows_workspace_size(_lib.TIDE_OP_SPARSE_ATTN, q.shape[0], self.dims,
-                                                         budget=sel.shape[2]),
-                   lambda ws: _lib.tide_sparse_attn(q, self.k_pool, self.v_pool, self.block_table, row_task, row_pos,
-                                                    sel, self.dims, out, lse, ws, stream))
+        ws = self._rows_workspace(_lib.TIDE_OP_SPARSE_ATTN, q.shape[0], sel.shape[-1])
+        _lib.tide_sparse_attn(q, self.k_pool, self.v_pool, self.block_table, row_task, row_pos, sel, self.dims, out, lse,
+                              ws, stream)
         return out
 
 

@@ -1,12 +1,12 @@
 """Memory of the calls whose rows and lengths are device data (needs an MI355X): which of a page map's arrays may be the
-same."""
+same, and workspaces that graphs use."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2608_10402_amd as tide
 import rows_reference as W
-from test_gpu_rows import dev, engine
+from test_gpu_rows import Sparse, dev, engine, rows_to_dev
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +43,36 @@ def test_page_map_refuses_to_replace_the_wanted_lengths(rows):
     lens, _, _, _, _, expect = W.page_map([0, 0], [60, 2000], np.zeros((2, 300)), [3, 2, 1, 0], 4, rows)
     assert lens == ([60, 0] if rows >= 60 else [0, 0]) and table.lens.tolist() == lens
     assert np.array_equal(np.stack([x.cpu().numpy() for x in out], 1), expect)
+
+
+def test_a_graph_keeps_its_workspace():
+    """A captured choice and attention of 64 rows, replayed after eager calls of fewer rows, whose split lists need
+    more memory, and of more: the results of the eager call each time, and nothing written to other tensors."""
+    s = Sparse(41, [4096, 4000], 28, 4, 128)
+    q, task, pos = s.rows(64)
+    q, task, pos = rows_to_dev(q), dev(task), dev(pos)
+    kv, bounds = s.p.kv, s.p.kv.new_bounds()
+    kv.key_bounds(dev(s.lens), bounds)
+
+    def call(n):
+        sel = kv.select_blocks(q[:n], task[:n], pos[:n], bounds, 128, 1, 2, out=torch.full((n, 4, 128), -1, device="cuda",
+                                                                                          dtype=torch.int32))
+        return sel, kv.sparse(q[:n], task[:n], pos[:n], sel)
+
+    want = call(64)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = call(64)
+    few = call(32)
+    more = torch.cat([q] * 40), torch.cat([task] * 40), torch.cat([pos] * 40)
+    for i in range(3):
+        filler = [torch.full((1 << k,), 7, dtype=torch.uint8, device="cuda") for k in range(8, 25)]
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+        assert all((x == 7).all() for x in filler), i
+        for x in got:
+            x.fill_(3)
+        assert all(torch.equal(a, b) for a, b in zip(call(32), few)), i
+        kv.select_blocks(*more, bounds, 128, 1, 2)
+        torch.zeros(1000, device="cuda").sum().item()
