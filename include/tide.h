@@ -488,7 +488,9 @@ TIDE_API int tide_kv4_evict(void* kv4_pool, float* mass_pool, int64_t num_pages,
  *   key bounds   int8 bounds[num_pages][num_kv_heads][2][head_dim] and units[num_pages][num_kv_heads]: with s the
  *                least integer in [-120, 122] such that max|k| <= 127 * 2^s over a page's positions and
  *                entries, bounds[.][.][0] = ceil(max of k / 2^s) and [1] = floor(min of k / 2^s), entry by
- *                entry, units = s; a page with a key that is not finite has unit 127 and zeros
+ *                entry, units = s; a page with a key that is not finite has unit 127 and zeros.  The positions
+ *                are those that the page held when its bounds were last brought up to date: tide_slot_append does
+ *                that for the pages it writes, tide_key_bounds for others
  *
  * Workspace: tide_rows_workspace_size; num_rows, budget and max_len as the call gets them (budget: attention;
  * max_len: selection, the longest context, > 0).  It holds nothing between calls.  Sizes are not monotone:
@@ -517,6 +519,9 @@ TIDE_API int tide_rows_workspace_bound(int op, int32_t num_rows, int32_t budget,
  * and the tasks before it need (refused ones too, for want of pages) are more than there are: then
  * lens_out == lens != want, its block-table row stays as it is, and its rows, if num_rows has room for them,
  * are padding.  A task whose lens or want is negative or above 16 * bt_stride is left alone, without rows.
+ * A task that is cut inside a page leaves that page the key bounds of what it held (a unit of 127 too, which
+ * outranks every finite score) until the next append to it; tide_key_bounds with from_lens = lens_out - 1
+ * brings the last page of every task up to date before a selection.
  * Entries of free_pages and of block_table that no page is put into keep what they hold.  A page that two
  * tasks share must not be given back by both.  num_tasks * bt_stride < 2^31 and num_rows < 2^31 - 1
  * (TIDE_ERR_UNSUPPORTED).  num_tasks == 0: nothing is written.
@@ -540,7 +545,8 @@ TIDE_API int tide_slot_append(const void* k_new, const void* v_new, const int64_
 
 /*
  * Key bounds of the pages that hold positions from_lens[b] .. lens[b] - 1 of each task (device int32; from_lens
- * NULL: 0), from all of a page's positions below lens[b]: for contexts that other calls wrote or moved.
+ * NULL: 0), from all of a page's positions below lens[b]: for contexts that other calls wrote or moved, and
+ * for pages that tide_page_map cut.
  * Bounds of other pages stay as they are, and of a page id out of range none are written.  max_len: no
  * position at or past it is looked at (0: 16 * bt_stride, and at most that, else TIDE_ERR_CAPACITY); the call's
  * time grows with it.  Tasks that share a page and fill it differently: either's bounds.

@@ -227,7 +227,8 @@ class PagedKV(_Paged):
 
     def key_bounds(self, lens, bounds, from_lens=None, max_len: int = 0, stream=None):
         """Key bounds of the pages that hold positions from_lens (None: 0) .. lens - 1 of each task, both on
-        the device (tide_key_bounds): after append, extend_append, evict and what else writes keys."""
+        the device (tide_key_bounds): after append, extend_append, evict and what else writes keys, and, with
+        from_lens = lens - 1, after a PageTable.map that cut contexts inside a page."""
         _lib.tide_key_bounds(self.k_pool, self.block_table, lens, bounds[0], bounds[1], self.dims, from_lens, max_len,
                              self._rows_workspace(_lib.TIDE_OP_KEY_BOUNDS, 0), stream)
         return bounds
@@ -280,7 +281,8 @@ class PageTable:
     def map(self, want_lens, rows, stream=None):
         """Bring every task's length to want_lens (device int32 [num_tasks]), taking pages or giving them
         back (tide_page_map), and put the new tokens into rows (from new_rows).  A task that is refused
-        keeps its length: lens != want_lens."""
+        keeps its length: lens != want_lens.  One that is cut inside a page leaves that page its key bounds
+        until the next append to it: PagedKV.key_bounds(lens, bounds, from_lens=lens - 1) renews them."""
         _lib.tide_page_map(self.lens, want_lens, self.block_table, self.free_pages, self.free_count, self.lens,
                            self.free_count, self.row_start, rows[0], rows[1], rows[2], self._dims, stream)
         return rows

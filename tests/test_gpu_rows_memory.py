@@ -1,12 +1,12 @@
 """Memory of the calls whose rows and lengths are device data (needs an MI355X): which of a page map's arrays may be the
-same, and workspaces that graphs use."""
+same, workspaces that graphs use, and the bounds of pages that were cut."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2608_10402_amd as tide
 import rows_reference as W
-from test_gpu_rows import Sparse, dev, engine, rows_to_dev
+from test_gpu_rows import D, HKV, HQ, Sparse, dev, engine, host, rows_to_dev
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +76,53 @@ def test_a_graph_keeps_its_workspace():
         assert all(torch.equal(a, b) for a, b in zip(call(32), few)), i
         kv.select_blocks(*more, bounds, 128, 1, 2)
         torch.zeros(1000, device="cuda").sum().item()
+
+
+@pytest.mark.parametrize("by", ["key_bounds", "append"])
+def test_bounds_of_a_page_that_was_cut(by):
+    """A context that ends inside a page leaves the page the bounds of what it held, here of a key that is not a
+    number and of a large one; from_lens = lens - 1 brings the last pages up to date, as the next append does."""
+    rng = np.random.default_rng(42)
+    kv, table, bounds = engine(3, 20, 60)
+    lens, cut = [200, 110, 96], [165, 83, 96]  # inside pages 10 and 5; the third stays
+    rows = table.new_rows(sum(lens))
+    table.map(dev(lens), rows)
+    k = rng.standard_normal((sum(lens), HKV, D))
+    k[180:200], k[200 + 90] = 1e6, np.nan  # positions 180 .. of the first task, 90 of the second
+    k = rows_to_dev(k)
+    kv.append_slots(k, k, rows[2], bounds)
+    before = [x.cpu().numpy() for x in bounds]
+    table.map(dev(cut), table.new_rows(0))
+    q = rows_to_dev(rng.standard_normal((3, HQ, D)))
+    task, pos = dev([0, 1, 2]), dev([x - 1 for x in cut])
+
+    # what the cut leaves: the bounds as they were, which a choice goes by
+    bt, g = table.block_table.cpu().numpy(), HQ // HKV
+    assert (before[1][bt[1, 5]] == W.NONE).all()
+    assert (kv.select_blocks(q, task, pos, bounds, 2)[1] == 5).any(-1).all()
+
+    held, last = host(kv.k_pool), list(cut)
+    if by == "key_bounds":
+        kv.key_bounds(table.lens, bounds, from_lens=table.lens - 1)
+    else:
+        rows, one = table.new_rows(3), rows_to_dev(rng.standard_normal((3, HKV, D)))
+        last = [x + 1 for x in cut]
+        table.map(dev(last), rows)
+        kv.append_slots(one, one, rows[2], bounds)
+        bt, held, pos = table.block_table.cpu().numpy(), host(kv.k_pool), dev([x - 1 for x in last])
+    after = [x.cpu().numpy() for x in bounds]
+    changed = {int(bt[b, (n - 1) // 16]) for b, n in enumerate(last)}
+    for page in range(60):
+        if page not in changed:
+            assert np.array_equal(after[0][page], before[0][page]) and np.array_equal(after[1][page], before[1][page])
+    for b, n in enumerate(last):
+        page = bt[b, (n - 1) // 16]
+        for h in range(HKV):
+            hi, lo, s = W.bounds_of(held[page, h, : (n - 1) % 16 + 1])
+            assert after[1][page, h] == s and np.array_equal(after[0][page, h], np.stack((hi, lo)))
+    sel, hq = kv.select_blocks(q, task, pos, bounds, 4, 1, 0).cpu().numpy(), host(q)
+    for b, n in enumerate(last):
+        at = bt[b, : W.pages_of(n)]
+        for h in range(HKV):
+            s = W.scores(hq[b, h * g:(h + 1) * g], after[0][at, h, 0], after[0][at, h, 1], after[1][at, h])
+            assert sel[b, h].tolist() == W.choose(s, len(at), 4, 1, 0)
