@@ -568,7 +568,8 @@ TIDE_API int tide_key_bounds(const void* k_pool, int64_t num_pages, const int32_
  * which is exact (no key's product with the whole-number query exceeds it); equal scores: the earlier block.
  * A block of unit 127 scores +inf, one whose page id is out of range -inf; a query head with a NaN or an
  * infinity counts as zeros.  max_len: rows at positions at or past it are padding (0: 16 * bt_stride, and at
- * most that, else TIDE_ERR_CAPACITY); workspace and time grow with it.
+ * most that, else TIDE_ERR_CAPACITY); workspace and time grow with it.  This and tide_sparse_attn choose their
+ * kernels by num_rows (padding counts) against num_tasks; a table of about the tasks that have rows is fastest.
  */
 TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int32_t* row_pos, int32_t num_rows,
                       const int8_t* bounds, const int8_t* units, int64_t num_pages,

@@ -81,6 +81,10 @@ constexpr int64_t kScoreRowWaves = 8192, kScoreChunkWaves = 4096;
 // and choice, row by row and task by task: 28 / 4 heads, 64 x 4 rows 43 and 44 us, 64 x 8 64 and 52, 8 x 4 16 and 31, 8 x
 // 16 30 and 19, 256 x 2 85 and 124, 256 x 4 154 and 102; 8 / 8 heads, whose products hold four times the rows, 64 x 4 61
 // and 238, 64 x 8 111 and 130, 64 x 16 243 and 91, 256 x 4 298 and 284.)
+// Launches may not depend on device data, so what counts is the table's height and the rows with their padding: in a table
+// much taller than the tasks that have rows, or a batch that is mostly padding, this is the slower one of the two (32 / 8
+// heads, contexts of 1k-16k: 256 single tokens of 256 tasks 66 us, with 1,792 rows of padding behind them 364; 8 x 128 rows
+// of 4k-16k 55 in tables of 8-256 tasks, 133 of 1,056).  A table of the tasks that have rows avoids it.
 bool score_by_task(int32_t num_rows, int32_t num_tasks, int32_t group) {
   const int64_t rows = num_rows, tasks = num_tasks;
   return rows >= (group > 2 ? 8 : 16) * tasks || (rows >= 4 * tasks && rows >= 1024);
@@ -149,7 +153,8 @@ size_t sparse_bound(int32_t num_rows, int32_t budget, const tide_dims& dims) {
 
 // Up to this many (row, kv head) pairs rows are taken one by one even where they share a task: a workgroup each, all at
 // once (28 / 4 heads, 128 blocks, 64 rows of a task: 18 us, 31 together; 8 x 16 rows 31 and 35; 8 x 64 rows 103 and 52;
-// 32 / 8 heads, 8 x 16 rows: 55 and 40).
+// 32 / 8 heads, 8 x 16 rows: 55 and 40).  Whether rows share tasks goes by the table's height, as above: 8 x 128 rows take
+// 194 us in tables of 8-256 tasks, 650 of 1,056, and 256 single tokens 318, with 256 rows of padding 352.
 constexpr int64_t kFewPairs = 512;
 
 // Rows that a workgroup takes at once: 1 where rows have tasks of their own or are few, and where their lists or

@@ -318,7 +318,7 @@ void sparse_shared_kernel(SparseArgs a) {
           for (int e = 0; e < 2; ++e) {
             const float x0 = fast_exp2(fmaf(s[u][t][2 * e], a.scale_log2, t ? off1 : off0));
             const float x1 = fast_exp2(fmaf(s[u][t][2 * e + 1], a.scale_log2, t ? off1 : off0));
-            // weights go to the P V product in bf16; the sum that divides it is of the rounded ones
+            // weights go to the P V product in bf16; the sum that divides it is of the rounded ones (sparse_attn.hip)
             wp[2 * t + e] = pack_bf16x2(x0, x1);
             l_part[u] = add_bf16x2(wp[2 * t + e], l_part[u]);
             l_exact[u] += x0 + x1;
