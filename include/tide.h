@@ -581,7 +581,7 @@ TIDE_API int tide_block_select(const void* q, const int32_t* row_task, const int
  * Attention of each row over the positions at or before its own in the blocks that sel[row][KV head] lists,
  * in any order; an entry that is negative, past the row's position or whose page id is out of range
  * adds nothing, and a block listed twice counts twice.  budget <= 2^30 (TIDE_ERR_UNSUPPORTED; so for
- * tide_block_select).  q/out: bf16 [num_rows][Hq][d]; lse: fp32
+ * tide_block_select).  q/out: bf16 [num_rows][Hq][d], which must not overlap (TIDE_ERR_INVALID_ARG); lse: fp32
  * [num_rows][Hq] or NULL.  A row of which no entry adds anything gets zeros, and an lse of -inf.
  */
 TIDE_API int tide_sparse_attn(const void* q, const void* k_pool, const void* v_pool, int64_t num_pages,

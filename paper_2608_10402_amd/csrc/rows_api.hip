@@ -410,6 +410,10 @@ TIDE_API int tide_sparse_attn(const void* q, const void* k_pool, const void* v_p
     if (!on16(q) || !on16(k_pool) || !on16(v_pool) || !on16(out) || !on16(workspace)) return TIDE_ERR_INVALID_ARG;
     size_t ml_off = 0;
     if (workspace_bytes < sparse_bytes(num_rows, budget, *dims, &ml_off)) return TIDE_ERR_CAPACITY;
+    // (rows that are taken again read q after out was written)
+    const uintptr_t q_at = reinterpret_cast<uintptr_t>(q), out_at = reinterpret_cast<uintptr_t>(out);
+    if ((q_at < out_at ? out_at - q_at : q_at - out_at) < (uintptr_t)num_rows * dims->num_q_heads * dims->head_dim * 2)
+      return TIDE_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     rc = clear_flags(workspace, s);
     if (rc != TIDE_OK) return rc;

@@ -195,3 +195,9 @@ def test_a_choice_past_the_table_takes_no_memory(monkeypatch):
     with pytest.raises(tide.TideError):
         e.select(1, 2**31 - 1)
     assert e.append().numel() < 1 << 22
+
+
+@pytest.mark.parametrize("out", [1 << 24, (1 << 24) + 3 * 28 * 128 * 2 - 16, (1 << 24) - 3 * 28 * 128 * 2 + 16])
+def test_attention_over_lists_refuses_outputs_over_queries(out):
+    """Rows that are taken again read their queries after outputs were written."""
+    assert call("tide_sparse_attn", q=1 << 24, out=out) == tide.TIDE_ERR_INVALID_ARG
